@@ -283,6 +283,119 @@ int duo_deferred_sample(const float *logits, const float *root_logits, int vocab
                         void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * ---- Many requests on a paged cache.
+ *
+ * duo_verify serves one request whose cache is one plane of max_seq slots.  A server holds many requests of very
+ * different lengths: their keys and values lie in PAGES of a common pool, and a step of all of them is
+ *
+ *   duo_page_plan -> for every layer (duo_page_append -> duo_page_attention) -> sampling -> duo_page_commit
+ *
+ * with the projections in between as the caller makes them.  A request has `cached` tokens in the cache and brings new
+ * rows: `trunk` tokens in a row (the token emitted last, a prompt or a part of one), then n branches of k draft tokens,
+ * each a continuation of the trunk (n * k = 0: none).  Its new rows are consecutive rows of the step's matrices, trunk
+ * first, then branch after branch; row t lies in the request's logical slot cached + t and has the rotary position
+ * cached + t in the trunk, cached + trunk + j for token j of a branch.  A row sees the request's cached slots, the trunk up
+ * to itself and the tokens of its own branch up to itself.  trunk = n * k = 0 is a request that sits this step out.
+ *
+ * Logical slot s of request r is slot s % page_slots of page block_table[r][s / page_slots].  Inside a page the planes
+ * [n_kv_heads][page_slots * head_dim] hold the tiles described at duo_kv_cache (duo_k_cache_offset / duo_v_cache_offset
+ * with the slot in the page).
+ *
+ * What the lengths ask for is decided on the device from the arrays of duo_page_batch: calls are sized by the batch's
+ * maxima alone, so a captured graph of a step serves steps of other lengths.  What only the device can see is reported in
+ * batch.status (DUO_PAGE_* bits, cleared by duo_page_plan):
+ *   a plan that fails (NO_PAGES, BAD_REQUEST) changes no table, takes no page, sets every slot and position to -1, and the
+ *   calls behind it do nothing, until a plan succeeds;
+ *   a page id outside the pool (BAD_PAGE) is not followed: its keys and values are not written, and reads take page 0
+ *   instead (the request's output is then of no use);
+ *   a workspace that holds no plan of this batch and geometry (NO_PLAN): the call does nothing;
+ *   a commit record that names no branch of its request (BAD_RECORD): nothing of that request is committed.
+ */
+#define DUO_PAGE_NO_PAGES    4  /* fewer free pages than the step needs */
+#define DUO_PAGE_BAD_REQUEST 8  /* a length or count of the batch or the tables is negative or beyond its maximum */
+#define DUO_PAGE_BAD_PAGE   16
+#define DUO_PAGE_NO_PLAN    32
+#define DUO_PAGE_BAD_RECORD 64
+
+#define DUO_PAGE_MAX_REQUESTS 4096
+#define DUO_PAGE_MAX_ROWS     262144   /* rows of a step */
+#define DUO_PAGE_MAX_SLOTS    8388608  /* slots of a request: max_pages * page_slots */
+
+typedef struct duo_page_cache {
+    uint16_t *k, *v;         /* [n_layers][n_pages][n_kv_heads][page_slots * head_dim] each, 16-byte aligned */
+    int32_t n_pages;         /* n_pages * page_slots < 2^31 */
+    int32_t page_slots;      /* 32, 64, 128, ... 1024 */
+    int32_t max_pages;       /* columns of the block table: the most pages of a request */
+} duo_page_cache;
+
+/* Who holds which page.  A caller starts with held = 0 everywhere and free_pages = all page ids in any order. */
+typedef struct duo_page_tables {
+    int32_t *block_table;    /* [n_requests][max_pages]; columns from held[r] on are neither read nor written */
+    int32_t *held;           /* [n_requests] pages of the request */
+    int32_t *free_pages;     /* [n_pages] a stack; entries from *free_count on are neither read nor written */
+    int32_t *free_count;     /* [1] */
+} duo_page_tables;
+
+typedef struct duo_page_batch {
+    const int32_t *cached, *trunk, *n, *k;  /* [n_requests] */
+    int32_t *row_start;      /* [n_requests + 1] by duo_page_plan: first row of every request, then the rows in all */
+    int32_t *position;       /* [max_rows] by duo_page_plan: rotary position of a row, -1 behind the last row */
+    int32_t *slot;           /* [max_rows] by duo_page_plan: page * page_slots + slot in the page, -1 behind the last row */
+    int32_t *status;         /* [1] */
+    int32_t n_requests;      /* rows of the block table, at most DUO_PAGE_MAX_REQUESTS */
+    int32_t max_rows;        /* rows of the step's matrices, at most DUO_PAGE_MAX_ROWS */
+    int32_t max_new;         /* the most new rows of a request, at most max_rows */
+} duo_page_batch;
+
+/* Bytes of workspace of the calls below for this geometry (the fields of batch that count are n_requests, max_rows and
+ * max_new; the pointers of cache and batch are not looked at).  duo_page_plan leaves the step's schedule in it, which duo_page_attention
+ * and duo_page_commit read: one workspace per step in flight. */
+int duo_page_workspace_bytes(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_batch *batch, size_t *bytes);
+
+/*
+ * Plans a step: every request gets exactly the ceil((cached + new rows) / page_slots) pages it needs.  Requests that hold
+ * more (rejected branches, a request that has ended: cached = trunk = n * k = 0) release their last columns.  With F free
+ * pages the released ones (requests in order, columns ascending) are pushed behind them; missing pages are popped from
+ * that stack in the order in which requests and columns ask for them.  Writes row_start, position, slot and status of the batch and
+ * the schedule in the workspace.  `to` may be `from` (in place); otherwise the two share no memory, and `from` is left as it is.
+ */
+int duo_page_plan(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_tables *from, const duo_page_tables *to,
+                  const duo_page_batch *batch, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Rotates queries and keys of max_rows rows to their positions and writes keys and values into the pages of `layer`: q
+ * [max_rows][n_q_heads * head_dim], k and v [max_rows][n_kv_heads * head_dim], each with its own distance between rows in elements (a
+ * multiple of 8; so they can be column ranges of one projection's output).  q_out as q; it may be q.  Rows whose slot is -1
+ * are left out, in q_out too.  Only position, slot, status and max_rows of the batch are read.  The rotation is computed in
+ * fp32 from angles reduced in double precision, and rounded once.
+ */
+int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_batch *batch, int layer,
+                    const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
+                    uint16_t *q_out, int64_t q_out_stride, void *hip_stream);
+
+/*
+ * out = softmax(scale q K^T) V of every row of the planned step over what it sees (grouped heads: query head h reads kv
+ * head h / (n_q_heads / n_kv_heads)).  q and out as above; out shares no memory with q; rows of out behind the step's last
+ * row are left as they are.  scale > 0, or 0 for 1 / sqrt(head_dim).  Scores, maxima, sums and outputs are fp32; softmax weights
+ * enter the second product in the 16-bit type, as pairs (hi + lo) for requests of at most 64 rows * heads of a group,
+ * once rounded beyond; the output is rounded once.  What a row does not see does not touch it, infinities and NaN included.
+ */
+int duo_page_attention(const duo_model_config *cfg, const duo_page_cache *cache, const int32_t *block_table, const duo_page_batch *batch,
+                       int layer, const uint16_t *q, int64_t q_stride, uint16_t *out, int64_t out_stride, float scale,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Commits the planned step.  records int32 [n_requests][4] are commit records as duo_spec_sample writes them: {accepted
+ * branch or -1, its accepted tokens a, emitted token, ...}.  In every layer the keys and values of the branch's first a tokens
+ * move to the slots behind the trunk, and cached_out[r] = cached + trunk + a.  Branch -1: a = 0, the trunk alone is
+ * committed.  Branch and token both -1 (a sampling call that failed on the device), or a record that names no branch:
+ * cached_out[r] = cached.  Requests without branches commit their trunk whatever the record holds.  cached_out may be
+ * batch.cached.  Pages that are no longer needed are released by the next plan.
+ */
+int duo_page_commit(const duo_model_config *cfg, const duo_page_cache *cache, const int32_t *block_table, const duo_page_batch *batch,
+                    const int32_t *records, int32_t *cached_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * One skinny weight-streaming product, the building block of the target pass:
  * y[m][n] = sum_k x[m][k] * w[n][k]; x from duo_pack_activations (rows <= DUO_MAX_ROWS), w from
  * duo_pack_matrix (N x K, K % 32 == 0), y fp32 [rows][N] row-major.

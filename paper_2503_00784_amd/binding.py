@@ -23,13 +23,18 @@ SELECT_INDEPENDENT_LONGEST = 0
 SELECT_PAPER_SEQUENTIAL = 1
 STATUS_TOKEN_CLAMPED = 1
 STATUS_PREFIX_MISMATCH = 2
+PAGE_NO_PAGES, PAGE_BAD_REQUEST, PAGE_BAD_PAGE, PAGE_NO_PLAN, PAGE_BAD_RECORD = 4, 8, 16, 32, 64
+PAGE_MAX_REQUESTS = 4096
+PAGE_MAX_ROWS = 262144
+PAGE_MAX_SLOTS = 8388608
 
 EXPORTS = ["duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample_workspace_bytes",
            "duo_spec_sample", "duo_spec_sample_noalloc", "duo_verify_deferred", "duo_deferred_sample", "duo_skinny_gemm",
            "duo_block_gemm", "duo_stream_read_probe", "duo_k_cache_offset",
            "duo_v_cache_offset", "duo_status_string", "duo_last_hip_error", "duo_profile_enable",
            "duo_profile_read", "duo_profile_dropped", "duo_profile_kernel_name", "duo_packed_elems", "duo_pack_matrix", "duo_pack_qkv", "duo_pack_gate_up",
-           "duo_pack_activations"]
+           "duo_pack_activations",
+           "duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit"]
 NOALLOC_MAX_VOCAB = 131072
 PROF_CLASSES = ["setup", "qkv_rope", "attn", "attn_combine", "o_proj", "residual_reduce", "gate_up_swiglu", "down_proj", "lm_head",
                 "sample", "commit", "qkv_finish"]
@@ -61,6 +66,19 @@ class Call(C.Structure):
 class Result(C.Structure):
     _fields_ = [("accept_len", C.c_void_p), ("next_token", C.c_void_p), ("commit", C.c_void_p),
                 ("status", C.c_void_p), ("logits_out", C.c_void_p)]
+
+
+class PageCacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("page_slots", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class PageTablesC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("block_table", "held", "free_pages", "free_count")]
+
+
+class PageBatchC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("cached", "trunk", "n", "k", "row_start", "position", "slot", "status")] + \
+               [(n, C.c_int32) for n in ("n_requests", "max_rows", "max_new")]
 
 
 class DuoError(RuntimeError):
@@ -124,7 +142,15 @@ def load(dtype: str = "bf16") -> C.CDLL:
     lib.duo_pack_qkv.argtypes = [C.POINTER(ModelConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.duo_pack_gate_up.argtypes = [C.POINTER(ModelConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.duo_pack_activations.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
-    for name in ("duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample_workspace_bytes",
+    page = [C.POINTER(ModelConfig), C.POINTER(PageCacheC)]
+    lib.duo_page_workspace_bytes.argtypes = page + [C.POINTER(PageBatchC), C.POINTER(C.c_size_t)]
+    lib.duo_page_plan.argtypes = page + [C.POINTER(PageTablesC), C.POINTER(PageTablesC), C.POINTER(PageBatchC), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.duo_page_append.argtypes = page + [C.POINTER(PageBatchC), C.c_int] + [C.c_void_p, C.c_int64] * 4 + [C.c_void_p]
+    lib.duo_page_attention.argtypes = page + [C.c_void_p, C.POINTER(PageBatchC), C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_float,
+                                              C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.duo_page_commit.argtypes = page + [C.c_void_p, C.POINTER(PageBatchC), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    for name in ("duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit",
+                 "duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample_workspace_bytes",
                  "duo_spec_sample", "duo_verify_deferred", "duo_deferred_sample", "duo_skinny_gemm", "duo_block_gemm", "duo_pack_matrix",
                  "duo_pack_qkv", "duo_pack_gate_up", "duo_pack_activations"):
         getattr(lib, name).restype = C.c_int
@@ -446,6 +472,168 @@ class VerifyEngine:
         self.host_prefix_len = out["new_prefix_len"]  # the commit advanced the device-side prefix length
         out["device_prefix_len"] = int(extra[0])
         return out
+
+
+class PageTables:
+    """Who holds which page (duo_page_tables): int32 device tensors block_table [requests][max_pages], held [requests],
+    free_pages [n_pages], free_count [1]."""
+
+    def __init__(self, block_table, held, free_pages, free_count):
+        self.block_table, self.held, self.free_pages, self.free_count = block_table, held, free_pages, free_count
+
+    @classmethod
+    def empty(cls, requests: int, max_pages: int, n_pages: int, device) -> "PageTables":
+        """No request holds a page, every page is free."""
+        import torch
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((requests, max_pages), -1, **i32), torch.zeros(requests, **i32), torch.arange(n_pages - 1, -1, -1, **i32),
+                   torch.full((1,), n_pages, **i32))
+
+    def tensors(self):
+        return self.block_table, self.held, self.free_pages, self.free_count
+
+    def c(self) -> PageTablesC:
+        return PageTablesC(*[t.data_ptr() for t in self.tensors()])
+
+
+class PagedCache:
+    """Keys and values of many requests in pages of a common pool, and the calls of a step over them (the duo_page_* entry
+    points of include/duo_verify.h): plan, then append and attention for every layer, then commit.
+
+    The caller fills the int32 device tensors `cached`, `trunk`, `n` and `k` (or calls `set_requests`); `plan` leaves
+    `row_start`, `position`, `slot`, `status` and `tables`.  key_pages / value_pages hold the 16-bit patterns of the library
+    build that `dtype` names, [layers][pages][kv heads][page_slots * head_dim] in the cache's tiles.  Calls go to the current
+    stream of the cache's device, whatever device is current; one PagedCache holds the schedule of one step at a time."""
+
+    def __init__(self, shape, n_pages: int, max_requests: int, max_pages: int, max_rows: int, max_new: Optional[int] = None,
+                 page_slots: int = 64, dtype: str = "bf16", device: str = "cuda:0"):
+        import torch
+        self.torch = torch
+        self.shape, self.dtype = shape, dtype
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device() if self.device.type == "cuda" else 0)
+        self.lib = load(dtype)
+        self.cfg = make_config(shape, 32)
+        self.max_requests, self.max_rows = int(max_requests), int(max_rows)
+        self.max_new = self.max_rows if max_new is None else int(max_new)
+        self.n_pages, self.page_slots, self.max_pages = int(n_pages), int(page_slots), int(max_pages)
+        self.ws_bytes = self._workspace_bytes()  # refuses what the library does not take, before anything is allocated
+        i32 = dict(dtype=torch.int32, device=device)
+        dims = (shape.n_layers, self.n_pages, shape.n_kv_heads, self.page_slots * shape.head_dim)
+        self.key_pages = torch.zeros(dims, dtype=torch.int16, device=device)
+        self.value_pages = torch.zeros(dims, dtype=torch.int16, device=device)
+        self.tables = PageTables.empty(self.max_requests, self.max_pages, self.n_pages, device)
+        self.cached, self.trunk, self.n, self.k = (torch.zeros(self.max_requests, **i32) for _ in range(4))
+        self.row_start = torch.zeros(self.max_requests + 1, **i32)
+        self.position, self.slot = (torch.full((self.max_rows,), -1, **i32) for _ in range(2))
+        self.status = torch.zeros(1, **i32)
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
+        self._planned = self.max_requests
+
+    def _workspace_bytes(self) -> int:
+        out = C.c_size_t(0)
+        cache = PageCacheC(None, None, self.n_pages, self.page_slots, self.max_pages)
+        batch = PageBatchC(*[None] * 8, self.max_requests, self.max_rows, self.max_new)
+        _check(self.lib.duo_page_workspace_bytes(C.byref(self.cfg), C.byref(cache), C.byref(batch), C.byref(out)), "duo_page_workspace_bytes")
+        return out.value
+
+    def _cache_c(self) -> PageCacheC:
+        return PageCacheC(self.key_pages.data_ptr(), self.value_pages.data_ptr(), self.n_pages, self.page_slots, self.max_pages)
+
+    def _batch_c(self, n_requests: int) -> PageBatchC:
+        return PageBatchC(*[t.data_ptr() for t in (self.cached, self.trunk, self.n, self.k, self.row_start, self.position, self.slot, self.status)],
+                          n_requests, self.max_rows, self.max_new)
+
+    def _stream(self):
+        return self.torch.cuda.current_stream(self.device).cuda_stream
+
+    def _rows(self, name: str, t, heads: int, writes: bool = False):
+        """A matrix of the step's rows, [max_rows][heads * head_dim] or [max_rows][heads][head_dim], rows any distance apart: (pointer, distance)."""
+        D = self.shape.head_dim
+        want = self.torch.float16 if self.dtype == "fp16" else self.torch.bfloat16
+        if t.dtype not in (want, self.torch.int16) or t.device != self.device:
+            raise ValueError(f"{name} must be {want} or int16 bit patterns on {self.device}, not {t.dtype} on {t.device}")
+        if tuple(t.shape) not in ((self.max_rows, heads * D), (self.max_rows, heads, D)):
+            raise ValueError(f"{name} must be [{self.max_rows}][{heads} * {D}], not {list(t.shape)}")
+        if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != D):
+            raise ValueError(f"{name}: the elements of a row must lie together")
+        stride = t.stride(0) if self.max_rows > 1 else heads * D
+        if writes and stride < heads * D:
+            raise ValueError(f"{name}: rows overlap")
+        return t.data_ptr(), stride
+
+    def _ints(self, name: str, t, dims):
+        if t.dtype != self.torch.int32 or t.device != self.device or tuple(t.shape) != tuple(dims) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous int32 {list(dims)} on {self.device}, not {t.dtype} {list(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def set_requests(self, trunk: Sequence[int], n: Sequence[int], k: Sequence[int], cached: Optional[Sequence[int]] = None) -> None:
+        """What the requests bring to the next step, from the host; `cached` only where it is not what the commits left."""
+        for dst, src in ((self.trunk, trunk), (self.n, n), (self.k, k), (self.cached, cached)):
+            if src is not None:
+                src = self.torch.tensor(list(src), dtype=self.torch.int32)
+                if len(src) > self.max_requests:
+                    raise ValueError(f"{len(src)} requests, the cache has room for {self.max_requests}")
+                dst[:len(src)] = src.to(self.device)
+
+    def _count(self, n_requests: Optional[int]) -> int:
+        n = self.max_requests if n_requests is None else int(n_requests)
+        if not 1 <= n <= self.max_requests:
+            raise ValueError(f"{n} requests, the cache has room for {self.max_requests}")
+        return n
+
+    def plan(self, n_requests: Optional[int] = None, source: Optional[PageTables] = None) -> None:
+        """Enqueue the plan of a step of the first n_requests requests.  `source`: the tables to start from, left as they are
+        (`tables` receives the result); default `tables`, in place."""
+        n = self._count(n_requests)
+        src = self.tables if source is None else source
+        for t in (src, self.tables):
+            self._ints("block_table", t.block_table, (self.max_requests, self.max_pages))
+            self._ints("held", t.held, (self.max_requests,))
+            self._ints("free_pages", t.free_pages, (self.n_pages,))
+            self._ints("free_count", t.free_count, (1,))
+        with self.torch.cuda.device(self.device):
+            rc = self.lib.duo_page_plan(C.byref(self.cfg), C.byref(self._cache_c()), C.byref(src.c()), C.byref(self.tables.c()), C.byref(self._batch_c(n)),
+                                        self.workspace.data_ptr(), self.ws_bytes, self._stream())
+        _check(rc, "duo_page_plan")
+        self._planned = n
+
+    def append(self, layer: int, q, k, v, q_out=None):
+        """Enqueue the rotary embedding of q and k and the writing of k and v into the pages; returns q_out (default: in place)."""
+        q_out = q if q_out is None else q_out
+        hq, hkv = self.shape.n_q_heads, self.shape.n_kv_heads
+        args = [x for t in (self._rows("q", q, hq), self._rows("k", k, hkv), self._rows("v", v, hkv), self._rows("q_out", q_out, hq, True)) for x in t]
+        with self.torch.cuda.device(self.device):
+            rc = self.lib.duo_page_append(C.byref(self.cfg), C.byref(self._cache_c()), C.byref(self._batch_c(self._planned)), int(layer), *args, self._stream())
+        _check(rc, "duo_page_append")
+        return q_out
+
+    def attention(self, layer: int, q, out=None, scale: float = 0.0):
+        """Enqueue the attention of the planned rows (rotated queries, as `append` leaves them); returns out."""
+        hq = self.shape.n_q_heads
+        if out is None:
+            out = self.torch.zeros_like(q, memory_format=self.torch.contiguous_format)
+        args = [x for t in (self._rows("q", q, hq), self._rows("out", out, hq, True)) for x in t]
+        with self.torch.cuda.device(self.device):
+            rc = self.lib.duo_page_attention(C.byref(self.cfg), C.byref(self._cache_c()), self.tables.block_table.data_ptr(),
+                                             C.byref(self._batch_c(self._planned)), int(layer), *args, float(scale), self.workspace.data_ptr(),
+                                             self.ws_bytes, self._stream())
+        _check(rc, "duo_page_attention")
+        return out
+
+    def commit(self, records, cached_out=None) -> None:
+        """Enqueue the commit: records int32 [requests][4] as the samplers write them; the new lengths go to `cached`, or to cached_out."""
+        out = self.cached if cached_out is None else cached_out
+        self._ints("records", records, (self._planned, 4))
+        self._ints("cached_out", out, (out.shape[0],))
+        if out.shape[0] < self._planned:
+            raise ValueError(f"cached_out has room for {out.shape[0]} of {self._planned} requests")
+        with self.torch.cuda.device(self.device):
+            rc = self.lib.duo_page_commit(C.byref(self.cfg), C.byref(self._cache_c()), self.tables.block_table.data_ptr(),
+                                          C.byref(self._batch_c(self._planned)), records.data_ptr(), out.data_ptr(), self.workspace.data_ptr(),
+                                          self.ws_bytes, self._stream())
+        _check(rc, "duo_page_commit")
 
 
 def spec_sample(logits, root_logits, draft_tokens, draft_probs, uniforms, temperature: float = 1.0,

@@ -15,6 +15,7 @@
 #include "duo_common.h"
 #include "duo_gemm.h"
 #include "duo_gemm_block.h"
+#include "duo_internal.h"
 #include "duo_launch.h"
 #include "duo_pack.h"
 #include "duo_rowops.h"
@@ -625,6 +626,9 @@ int spec_sample_on_scratch(const float* logits, const float* root_logits, int vo
 }
 
 }  // namespace
+
+int duo_internal_hip_ok(hipError_t e, const char* what) { return hip_ok(e, what); }
+int duo_internal_check_config(const duo_model_config* c) { return check_config(c); }
 
 extern "C" {
 

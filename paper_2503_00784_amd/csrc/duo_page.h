@@ -1,0 +1,440 @@
+// Many requests on a paged cache: the plan of a step, the append of its keys and values, the commit of accepted branches.
+#pragma once
+#include "../../include/duo_verify.h"
+#include "duo_common.h"
+#include "duo_page_rules.h"
+
+// ---- what a plan leaves in the workspace (page_layout gives the places)
+struct PageHeader {  // one, PAGE_HEADER_INTS
+    int32_t magic, ok;
+    int32_t requests, hq, hkv, head_dim, page_slots, max_pages, max_rows, max_new;  // what the plan was made for
+    int32_t stream_items, tile_items, merges;
+    int32_t rows, free_in, free_out, released;
+};
+constexpr int32_t PAGE_MAGIC = 0x70616765;
+static_assert(sizeof(PageHeader) <= PAGE_HEADER_INTS * 4, "the header has its place");
+
+struct __align__(16) PageInfo {  // one per request
+    int32_t cached, trunk, n, k;
+    int32_t row0, rows, held, need;
+    int32_t take0, rel0;         // pages taken and released by the requests before it
+    int32_t item0, chunks;       // its first item (of its kind) and the key ranges per tile
+    int32_t part0, merge0;       // first partial result and first merge, if its tiles are cut
+    int32_t tiles, streamed;
+};
+static_assert(sizeof(PageInfo) == PAGE_INFO_INTS * 4, "the place of a request");
+
+struct __align__(16) PageItem {  // one workgroup per item and kv head
+    int32_t request, cached, trunk, k;
+    int32_t row0;                // the request's first row in the step's matrices
+    int32_t first, count;        // the tile's rows: pairs (token, query head of the group), first of them and how many
+    int32_t block0, blocks;      // key range
+    int32_t slots;               // cached + new rows
+    int32_t part;                // partial result, or -1: the item is its tile's only one and writes the output
+    int32_t last_block;          // of the request
+    int32_t pad[4];
+};
+static_assert(sizeof(PageItem) == PAGE_ITEM_INTS * 4, "the place of an item");
+
+struct __align__(16) PageMerge {  // a tile whose keys were cut
+    int32_t row0, first, count, part0, parts, streamed, pad[2];
+};
+static_assert(sizeof(PageMerge) == PAGE_MERGE_INTS * 4, "the place of a merge");
+
+struct PagePlanArgs {
+    const int32_t *cached, *trunk, *n, *k;
+    const int32_t *table_in, *held_in, *free_in, *count_in;
+    int32_t *table_out, *held_out, *free_out, *count_out;
+    int32_t *row_start, *position, *slot, *status;
+    int32_t requests, max_rows, max_new, n_pages, page_shift, max_pages;
+    int32_t hq, hkv, head_dim;
+    char* ws;
+    PageLayout lay;
+};
+
+// Exclusive sums of N quantities over the threads of a workgroup of up to 1024, and their totals.
+template <int N>
+__device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], int (*lds)[16]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) >> 6;
+    int own[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) own[i] = v[i];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        int up[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) up[i] = __shfl_up(v[i], o, 64);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += lane >= o ? up[i] : 0;
+    }
+    __syncthreads();
+    if (lane == 63) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[i][wave] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        int before = 0, all = 0;
+        for (int w = 0; w < waves; ++w) {
+            const int x = lds[i][w];
+            before += w < wave ? x : 0;
+            all += x;
+        }
+        v[i] += before - own[i];
+        total[i] = all;
+    }
+}
+
+// Part one of a plan, one workgroup: checks, sums over the requests, how the attention is cut.  A thread takes PER consecutive requests.
+// What bounds it is the latency of a chain of a dozen dependent steps (loads, two scans, stores).
+constexpr int PAGE_PLAN_THREADS = 1024, PAGE_PLAN_PER = PAGE_MAX_REQUESTS / PAGE_PLAN_THREADS;
+
+__global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArgs a) {
+    __shared__ int scan[8][16];
+    __shared__ unsigned long long work[2];
+    __shared__ int bad;
+    PageHeader* const hdr = reinterpret_cast<PageHeader*>(a.ws);
+    PageInfo* const info = reinterpret_cast<PageInfo*>(a.ws + a.lay.info);
+    const int group = a.hq / a.hkv, page = 1 << a.page_shift, max_slots = a.max_pages << a.page_shift;
+    const int per = (a.requests + (int)blockDim.x - 1) / (int)blockDim.x;
+    if (threadIdx.x == 0) work[0] = work[1] = 0, bad = 0;
+    __syncthreads();
+
+    PageInfo p[PAGE_PLAN_PER];
+    int wrong = 0;
+    enum { ROWS, REL, TAKE, TILES_S, TILES_B, SUMS };
+    int sum[SUMS] = {};
+    unsigned long long ws = 0, wt = 0;
+#pragma unroll
+    for (int i = 0; i < PAGE_PLAN_PER; ++i) {
+        const int r = threadIdx.x * per + i;
+        p[i] = PageInfo{};
+        if (i >= per || r >= a.requests) continue;
+        PageInfo& q = p[i];
+        q.cached = a.cached[r], q.trunk = a.trunk[r], q.n = a.n[r], q.k = a.k[r], q.held = a.held_in[r];
+        const long long rows = (long long)q.trunk + (long long)q.n * q.k;
+        const bool fits = q.cached >= 0 && q.trunk >= 0 && q.n >= 0 && q.k >= 0 && rows <= a.max_new && q.cached + rows <= max_slots &&
+                          q.held >= 0 && q.held <= a.max_pages;
+        wrong |= !fits;
+        if (!fits) q.cached = q.trunk = q.n = q.k = 0, q.held = q.held < 0 ? 0 : q.held > a.max_pages ? a.max_pages : q.held;
+        q.rows = fits ? (int)rows : 0;
+        q.need = (q.cached + q.rows + page - 1) >> a.page_shift;
+        const PageWork w = page_work(q.cached, q.rows, group);
+        q.tiles = w.tiles, q.streamed = w.streamed;
+        sum[ROWS] += q.rows;
+        sum[REL] += q.held > q.need ? q.held - q.need : 0;
+        sum[TAKE] += q.need > q.held ? q.need - q.held : 0;
+        (w.streamed ? ws : wt) += (unsigned long long)w.tiles * w.blocks;
+    }
+    if (wrong) bad = 1;
+    if (ws) atomicAdd(&work[0], ws);  // whole numbers: the order does not matter
+    if (wt) atomicAdd(&work[1], wt);
+    int total[SUMS];
+    block_scan(sum, total, scan);  // its barriers stand between the atomics and the reads
+    int status = bad ? DUO_PAGE_BAD_REQUEST : 0;
+    const int F = *a.count_in;
+    if (F < 0 || F > a.n_pages || total[ROWS] > a.max_rows || total[REL] > a.n_pages - F) status |= DUO_PAGE_BAD_REQUEST;
+    else if (total[TAKE] > F + total[REL]) status |= DUO_PAGE_NO_PAGES;
+    const bool ok = status == 0;
+
+    // the cuts
+    const int range_s = page_range((long long)work[0], a.hkv, PAGE_STREAM_TARGET, PAGE_STREAM_MIN_BLOCKS);
+    const int range_t = page_range((long long)work[1], a.hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS);
+    enum { ITEM_S, ITEM_T, PART_S, PART_T, MERGE, CUTS };
+    int cut[CUTS] = {};
+#pragma unroll
+    for (int i = 0; i < PAGE_PLAN_PER; ++i) {
+        PageInfo& q = p[i];
+        if (q.tiles == 0 || !ok) continue;
+        const int blocks = (q.cached + q.rows + 31) / 32, range = q.streamed ? range_s : range_t;
+        q.chunks = (blocks + range - 1) / range;
+        const int items = q.tiles * q.chunks;
+        cut[q.streamed ? ITEM_S : ITEM_T] += items;
+        if (q.chunks > 1) cut[q.streamed ? PART_S : PART_T] += items, cut[MERGE] += q.tiles;
+    }
+    int cuts[CUTS];
+    block_scan(cut, cuts, scan);
+
+    if (threadIdx.x == 0) {
+        *hdr = PageHeader{PAGE_MAGIC, ok, a.requests, a.hq, a.hkv, a.head_dim, page, a.max_pages, a.max_rows, a.max_new,
+                          cuts[ITEM_S], cuts[ITEM_T], cuts[MERGE], ok ? total[ROWS] : 0, ok ? F : 0, ok ? F + total[REL] - total[TAKE] : 0,
+                          ok ? total[REL] : 0};
+        *a.status = status;
+        if (ok) *a.count_out = F + total[REL] - total[TAKE];
+        else if (a.count_out != a.count_in) *a.count_out = F;
+        a.row_start[a.requests] = ok ? total[ROWS] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < PAGE_PLAN_PER; ++i) {
+        const int r = threadIdx.x * per + i;
+        if (i >= per || r >= a.requests) continue;
+        PageInfo& q = p[i];
+        if (!ok) {  // nothing changes: no rows, the pages of before (a copy of the tables where `to` is not `from`)
+            if (a.held_out != a.held_in) a.held_out[r] = a.held_in[r];
+            a.row_start[r] = 0;
+            q = PageInfo{};
+            info[r] = q;
+            continue;
+        }
+        q.row0 = sum[ROWS], q.rel0 = sum[REL], q.take0 = sum[TAKE];
+        sum[ROWS] += q.rows;
+        sum[REL] += q.held > q.need ? q.held - q.need : 0;
+        sum[TAKE] += q.need > q.held ? q.need - q.held : 0;
+        const int items = q.tiles * q.chunks;
+        int& at = cut[q.streamed ? ITEM_S : ITEM_T];
+        q.item0 = at;
+        at += items;
+        q.part0 = -1;
+        if (q.chunks > 1) {
+            int& part = cut[q.streamed ? PART_S : PART_T];
+            q.part0 = part, q.merge0 = cut[MERGE];
+            part += items, cut[MERGE] += q.tiles;
+        }
+        info[r] = q;
+        a.held_out[r] = q.need;
+        a.row_start[r] = q.row0;
+    }
+}
+
+// Part two: everything that is as long as rows, pages or items.  blockIdx.x < requests: request blockIdx.x, its threads spread over
+// gridDim.y workgroups; the workgroups beyond copy the free stack and mark the rows behind the last.
+// In place this is safe: columns that are written ([held, need) of requests that grow) are read by nobody, columns that are read ([need, held)
+// of requests that shrink) are written by nobody, and the stack is read below its old count only and written from there on only.
+__device__ __forceinline__ int released_page(const PagePlanArgs& a, const PageInfo* info, int rank) {
+    int lo = 0, hi = a.requests - 1;  // the last request whose released pages start at or before rank and that has any there
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (info[mid].rel0 <= rank) lo = mid;
+        else hi = mid - 1;
+    }
+    return a.table_in[(size_t)lo * a.max_pages + info[lo].need + (rank - info[lo].rel0)];
+}
+
+__global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
+    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    const PageInfo* const info = reinterpret_cast<const PageInfo*>(a.ws + a.lay.info);
+    const int group = a.hq / a.hkv;
+    const int t0 = blockIdx.y * blockDim.x + threadIdx.x, step = gridDim.y * blockDim.x;
+    const bool copies = a.table_out != a.table_in;
+    if ((int)blockIdx.x >= a.requests) {
+        const int i0 = ((int)blockIdx.x - a.requests) * step + t0, all = ((int)gridDim.x - a.requests) * step;
+        for (int i = hdr.rows + i0; i < a.max_rows; i += all) a.position[i] = a.slot[i] = -1;
+        if (copies) {
+            const int kept = hdr.ok ? min(hdr.free_in, hdr.free_out) : min(max(*a.count_in, 0), a.n_pages);
+            for (int i = i0; i < kept; i += all) a.free_out[i] = a.free_in[i];
+        }
+        return;
+    }
+    const int r = blockIdx.x;
+    const int32_t* const line_in = a.table_in + (size_t)r * a.max_pages;
+    int32_t* const line = a.table_out + (size_t)r * a.max_pages;
+    if (!hdr.ok) {
+        if (copies) {
+            const int held = min(max(a.held_in[r], 0), a.max_pages);
+            for (int c = t0; c < held; c += step) line[c] = line_in[c];
+        }
+        return;
+    }
+    const PageInfo p = info[r];
+    const int top = hdr.free_in + hdr.released;
+    // the page of column c: kept, or popped from the free pages with the released ones behind them
+    auto page_of = [&](int c) {
+        if (c < p.held) return line_in[c];
+        const int x = top - 1 - (p.take0 + c - p.held);
+        return x < hdr.free_in ? a.free_in[x] : released_page(a, info, x - hdr.free_in);
+    };
+    for (int c = (copies ? 0 : p.held) + t0; c < p.need; c += step) line[c] = page_of(c);
+    for (int c = p.need + t0; c < p.held; c += step) {
+        const int x = hdr.free_in + p.rel0 + c - p.need;
+        if (x < hdr.free_out) a.free_out[x] = line_in[c];
+    }
+    for (int t = t0; t < p.rows; t += step) {
+        const int logical = p.cached + t;
+        a.position[p.row0 + t] = t < p.trunk ? logical : p.cached + p.trunk + (t - p.trunk) % p.k;
+        const int page = page_of(logical >> a.page_shift);
+        const bool known = (unsigned)page < (unsigned)a.n_pages;
+        a.slot[p.row0 + t] = known ? (page << a.page_shift) + (logical & ((1 << a.page_shift) - 1)) : -1;
+        if (!known) atomicOr(a.status, DUO_PAGE_BAD_PAGE);
+    }
+    // the items of the attention; late tiles see the most keys and go first
+    const int items = p.tiles * p.chunks;
+    PageItem* const out = reinterpret_cast<PageItem*>(a.ws + (p.streamed ? a.lay.stream : a.lay.tile)) + p.item0;
+    const int pairs = p.rows * group;
+    for (int i = t0; i < items; i += step) {
+        const int tile = p.tiles - 1 - i / p.chunks, chunk = i % p.chunks;
+        const int first = tile * PAGE_TILE_ROWS, count = p.streamed ? pairs : min(PAGE_TILE_ROWS, pairs - first);
+        const int blocks = page_tile_blocks(p.cached, first, count, group), length = page_chunk_blocks(blocks, p.chunks);
+        PageItem it;
+        it.request = r, it.cached = p.cached, it.trunk = p.trunk, it.k = p.k, it.row0 = p.row0, it.first = first, it.count = count;
+        it.block0 = chunk * length;
+        it.blocks = max(0, min(length, blocks - it.block0));
+        it.slots = p.cached + p.rows;
+        it.part = p.chunks > 1 ? p.part0 + tile * p.chunks + chunk : -1;
+        it.last_block = (it.slots - 1) >> 5;
+        it.pad[0] = it.pad[1] = it.pad[2] = it.pad[3] = 0;
+        out[i] = it;
+        if (p.chunks > 1 && chunk == 0) {
+            PageMerge m;
+            m.row0 = p.row0, m.first = first, m.count = count, m.part0 = p.part0 + tile * p.chunks, m.parts = (blocks + length - 1) / length;
+            m.streamed = p.streamed, m.pad[0] = m.pad[1] = 0;
+            reinterpret_cast<PageMerge*>(a.ws + a.lay.merge)[p.merge0 + tile] = m;
+        }
+    }
+}
+
+// ---- append
+struct PageAppendArgs {
+    const u16 *q, *k, *v;
+    u16* q_out;
+    size_t q_stride, k_stride, v_stride, q_out_stride;
+    u16 *kc, *vc;  // this layer's pages
+    const int32_t *position, *slot;
+    int32_t* status;
+    int32_t rows, hq, hkv, page_shift, n_pages;
+    double turns[64];  // theta^(-2d/D) / 2 pi: turns per position
+};
+
+// A thread takes eight channels and their eight rotary partners of one (row, head): two 16-byte loads and stores; K's eight channels of a
+// slot are one 16-byte piece of a tile.  The angle is reduced in double precision (position times turns keeps 2^-53 of up to
+// 2^23 positions), the sine and cosine of the remainder are fp32.
+template <int D>
+__global__ __launch_bounds__(256) void page_rope_kernel(PageAppendArgs a) {
+    constexpr int TPH = D / 16;  // threads per head
+    const int heads = a.hq + a.hkv;
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    const int part = (int)(i % TPH);
+    const long long j = i / TPH;
+    const int head = (int)(j % heads);
+    const long long row = j / heads;
+    if (row >= a.rows) return;
+    const int slot = a.slot[row];
+    if (slot < 0) return;
+    const int page = slot >> a.page_shift;
+    const bool bad = page >= a.n_pages;
+    const double pos = (double)a.position[row];
+    const u16* src = head < a.hq ? a.q + row * a.q_stride + head * D : a.k + row * a.k_stride + (head - a.hq) * D;
+    src += part * 8;
+    Frag8 x, y, xo, yo;
+    x.q = *reinterpret_cast<const u32x4*>(src);
+    y.q = *reinterpret_cast<const u32x4*>(src + D / 2);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const double t = pos * a.turns[part * 8 + e];
+        float s, c;
+        sincospif(2.0f * (float)(t - floor(t)), &s, &c);
+        const float xf = elem_to_f32(x.h[e]), yf = elem_to_f32(y.h[e]);
+        xo.h[e] = f32_to_elem(xf * c - yf * s);
+        yo.h[e] = f32_to_elem(yf * c + xf * s);
+    }
+    if (head < a.hq) {
+        u16* dst = a.q_out + row * a.q_out_stride + head * D + part * 8;
+        *reinterpret_cast<u32x4*>(dst) = xo.q;
+        *reinterpret_cast<u32x4*>(dst + D / 2) = yo.q;
+    } else if (!bad) {
+        const int in_page = slot & ((1 << a.page_shift) - 1);
+        u16* plane = a.kc + (((size_t)page * a.hkv + (head - a.hq)) << a.page_shift) * D;
+        *reinterpret_cast<u32x4*>(plane + k_cache_offset(D, in_page, part * 8)) = xo.q;
+        *reinterpret_cast<u32x4*>(plane + k_cache_offset(D, in_page, part * 8 + D / 2)) = yo.q;
+    } else if (part == 0) {
+        atomicOr(a.status, DUO_PAGE_BAD_PAGE);
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void page_values_kernel(PageAppendArgs a) {
+    constexpr int TPH = D / 8;
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    const int part = (int)(i % TPH);
+    const long long j = i / TPH;
+    const int head = (int)(j % a.hkv);
+    const long long row = j / a.hkv;
+    if (row >= a.rows) return;
+    const int slot = a.slot[row];
+    if (slot < 0) return;
+    const int page = slot >> a.page_shift, in_page = slot & ((1 << a.page_shift) - 1);
+    if (page >= a.n_pages) return;
+    Frag8 x;
+    x.q = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + head * D + part * 8);
+    u16* plane = a.vc + (((size_t)page * a.hkv + head) << a.page_shift) * D;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) plane[v_cache_offset(D, in_page, part * 8 + e)] = x.h[e];
+}
+
+// ---- commit
+struct PageCommitArgs {
+    u16 *kc, *vc;
+    const int32_t *cached, *table, *records;
+    int32_t *cached_out, *status;
+    int32_t requests, layers, hkv, page_shift, n_pages, max_pages, max_new, hq, head_dim, max_rows;
+    const char* ws;
+    size_t info;
+};
+
+__device__ __forceinline__ bool page_plan_is(const PageHeader& h, int requests, int hq, int hkv, int D, int page_shift, int max_pages, int max_rows, int max_new) {
+    return h.magic == PAGE_MAGIC && h.requests == requests && h.hq == hq && h.hkv == hkv && h.head_dim == D && h.page_slots == 1 << page_shift &&
+           h.max_pages == max_pages && h.max_rows == max_rows && h.max_new == max_new;
+}
+
+// One workgroup per (request, layer, kv head).  K: a slot's eight channels are a 16-byte piece; V: a channel's slots are two bytes each.  Source and
+// target share no slot (branch 0 lies where it belongs, branch i >= 1 starts i * k >= a slots further on).
+template <int D>
+__global__ __launch_bounds__(128) void page_commit_kernel(PageCommitArgs a) {
+    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    const int r = blockIdx.x, layer = blockIdx.y, head = blockIdx.z;
+    const bool first = layer == 0 && head == 0 && threadIdx.x == 0;
+    const bool known = page_plan_is(hdr, a.requests, a.hq, a.hkv, D, a.page_shift, a.max_pages, a.max_rows, a.max_new);
+    if (!known || !hdr.ok) {
+        if (first) {
+            if (!known) atomicOr(a.status, DUO_PAGE_NO_PLAN);
+            a.cached_out[r] = a.cached[r];
+        }
+        return;
+    }
+    const PageInfo p = reinterpret_cast<const PageInfo*>(a.ws + a.info)[r];
+    const int branch = a.records[4 * r], accepted = a.records[4 * r + 1], token = a.records[4 * r + 2];
+    const int branches = p.k > 0 ? p.n : 0;
+    int moved = 0, after = p.cached + p.trunk;
+    if (branches > 0) {
+        const bool none = branch < 0;
+        if (none ? token < 0 : false) after = p.cached;
+        else if (!none) {
+            if (branch >= branches || accepted < 0 || accepted > p.k) {
+                after = p.cached;
+                if (first) atomicOr(a.status, DUO_PAGE_BAD_RECORD);
+            } else {
+                after += accepted;
+                moved = branch > 0 ? accepted : 0;
+            }
+        }
+    }
+    if (first) a.cached_out[r] = after;
+    if (moved == 0) return;
+    const int to0 = p.cached + p.trunk, from0 = to0 + branch * p.k;
+    const int32_t* line = a.table + (size_t)r * a.max_pages;
+    const size_t layer_pages = (size_t)layer * a.n_pages;
+    auto plane = [&](u16* base, int logical, bool& fine) {
+        const int page = line[logical >> a.page_shift];
+        fine = (unsigned)page < (unsigned)a.n_pages;
+        return base + (((layer_pages + (fine ? page : 0)) * a.hkv + head) << a.page_shift) * D;
+    };
+    const int mask = (1 << a.page_shift) - 1;
+    constexpr int KP = D / 8;
+    for (int i = threadIdx.x; i < moved * KP; i += blockDim.x) {
+        const int j = i / KP, d = i % KP * 8;
+        bool ok0, ok1;
+        u16* const src = plane(a.kc, from0 + j, ok0);
+        u16* const dst = plane(a.kc, to0 + j, ok1);
+        if (ok0 && ok1)
+            *reinterpret_cast<u32x4*>(dst + k_cache_offset(D, (to0 + j) & mask, d)) =
+                *reinterpret_cast<const u32x4*>(src + k_cache_offset(D, (from0 + j) & mask, d));
+        else atomicOr(a.status, DUO_PAGE_BAD_PAGE);
+    }
+    for (int i = threadIdx.x; i < moved * D; i += blockDim.x) {
+        const int j = i / D, d = i % D;
+        bool ok0, ok1;
+        u16* const src = plane(a.vc, from0 + j, ok0);
+        u16* const dst = plane(a.vc, to0 + j, ok1);
+        if (ok0 && ok1) dst[v_cache_offset(D, (to0 + j) & mask, d)] = src[v_cache_offset(D, (from0 + j) & mask, d)];
+    }
+}

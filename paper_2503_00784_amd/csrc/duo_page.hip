@@ -1,0 +1,201 @@
+// C ABI of the paged-cache calls: host-side validation and launches (kernels in duo_page.h and duo_page_attn.h).
+#include "../../include/duo_verify.h"
+
+#include <math.h>
+
+#include "duo_internal.h"
+#include "duo_page.h"
+#include "duo_page_attn.h"
+
+namespace {
+
+int page_shift_of(int slots) {
+    for (int s = 5; s <= 10; ++s)
+        if (slots == 1 << s) return s;
+    return -1;
+}
+bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool off4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+// The sizes that every call is given: model, pages and batch maxima.
+int check_sizes(const duo_model_config* cfg, const duo_page_cache* cache, const duo_page_batch* b) {
+    if (const int rc = duo_internal_check_config(cfg)) return rc;
+    if (!cache || !b) return DUO_ERR_NULL;
+    if (cache->n_pages < 1 || page_shift_of(cache->page_slots) < 0 || cache->max_pages < 1) return DUO_ERR_SHAPE;
+    if ((int64_t)cache->n_pages * cache->page_slots > 0x7fffffff || (int64_t)cache->max_pages * cache->page_slots > DUO_PAGE_MAX_SLOTS) return DUO_ERR_SHAPE;
+    if (b->n_requests < 1 || b->n_requests > DUO_PAGE_MAX_REQUESTS || b->max_rows < 1 || b->max_rows > DUO_PAGE_MAX_ROWS || b->max_new < 1 ||
+        b->max_new > b->max_rows)
+        return DUO_ERR_SHAPE;
+    return DUO_OK;
+}
+
+PageLayout layout_of(const duo_model_config* cfg, const duo_page_cache* cache, const duo_page_batch* b) {
+    return page_layout(b->n_requests, b->max_rows, b->max_new, cache->max_pages * cache->page_slots / 32, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim);
+}
+
+int check_workspace(const PageLayout& lay, const void* ws, size_t bytes) {
+    if (!ws) return DUO_ERR_NULL;
+    if (off16(ws)) return DUO_ERR_ALIGN;
+    return bytes < lay.total ? DUO_ERR_WORKSPACE : DUO_OK;
+}
+
+int check_tables(const duo_page_tables* t) {
+    if (!t || !t->block_table || !t->held || !t->free_pages || !t->free_count) return DUO_ERR_NULL;
+    return off4(t->block_table) || off4(t->held) || off4(t->free_pages) || off4(t->free_count) ? DUO_ERR_ALIGN : DUO_OK;
+}
+
+int check_rows(const void* p, int64_t stride, int64_t width) {
+    if (!p) return DUO_ERR_NULL;
+    if (off16(p) || stride % 8) return DUO_ERR_ALIGN;
+    return stride < width ? DUO_ERR_SHAPE : DUO_OK;
+}
+
+size_t layer_elems(const duo_model_config* cfg, const duo_page_cache* c) { return (size_t)c->n_pages * cfg->n_kv_heads * c->page_slots * cfg->head_dim; }
+
+template <int D>
+void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStream_t s) {
+    PageAttnArgs st = a;
+    st.items = lay.stream;
+    const dim3 grid(lay.stream_items * a.hkv);
+    if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D, 1>), grid, dim3(256), s, st);
+    else if (lay.stream_rows <= 32) DUO_LAUNCH((page_stream_kernel<D, 2>), grid, dim3(256), s, st);
+    else if (lay.stream_rows <= 48) DUO_LAUNCH((page_stream_kernel<D, 3>), grid, dim3(256), s, st);
+    else DUO_LAUNCH((page_stream_kernel<D, 4>), grid, dim3(256), s, st);
+    if (lay.tile_items > 0) {
+        PageAttnArgs tl = a;
+        tl.items = lay.tile;
+        DUO_LAUNCH((page_tile_kernel<D>), dim3(lay.tile_items * a.hkv), dim3(512), s, tl);
+    }
+    if (lay.merges > 0)
+        DUO_LAUNCH((page_merge_kernel<D>), dim3(lay.merges * a.hkv, lay.tile_parts > 0 ? 16 : lay.stream_rows / 4), dim3(256), s, a);
+}
+
+}  // namespace
+
+extern "C" int duo_page_workspace_bytes(const duo_model_config* cfg, const duo_page_cache* cache, const duo_page_batch* batch, size_t* bytes) {
+    if (!bytes) return DUO_ERR_NULL;
+    if (const int rc = check_sizes(cfg, cache, batch)) return rc;
+    *bytes = layout_of(cfg, cache, batch).total;
+    return DUO_OK;
+}
+
+extern "C" int duo_page_plan(const duo_model_config* cfg, const duo_page_cache* cache, const duo_page_tables* from, const duo_page_tables* to,
+                             const duo_page_batch* b, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (const int rc = check_sizes(cfg, cache, b)) return rc;
+    if (const int rc = check_tables(from)) return rc;
+    if (const int rc = check_tables(to)) return rc;
+    // all four in place, or none
+    const int same = (from->block_table == to->block_table) + (from->held == to->held) + (from->free_pages == to->free_pages) + (from->free_count == to->free_count);
+    if (same != 0 && same != 4) return DUO_ERR_ARG;
+    if (!b->cached || !b->trunk || !b->n || !b->k || !b->row_start || !b->position || !b->slot || !b->status) return DUO_ERR_NULL;
+    if (off4(b->cached) || off4(b->trunk) || off4(b->n) || off4(b->k) || off4(b->row_start) || off4(b->position) || off4(b->slot) || off4(b->status))
+        return DUO_ERR_ALIGN;
+    const PageLayout lay = layout_of(cfg, cache, b);
+    if (const int rc = check_workspace(lay, workspace, workspace_bytes)) return rc;
+    PagePlanArgs a{};
+    a.cached = b->cached, a.trunk = b->trunk, a.n = b->n, a.k = b->k;
+    a.table_in = from->block_table, a.held_in = from->held, a.free_in = from->free_pages, a.count_in = from->free_count;
+    a.table_out = to->block_table, a.held_out = to->held, a.free_out = to->free_pages, a.count_out = to->free_count;
+    a.row_start = b->row_start, a.position = b->position, a.slot = b->slot, a.status = b->status;
+    a.requests = b->n_requests, a.max_rows = b->max_rows, a.max_new = b->max_new;
+    a.n_pages = cache->n_pages, a.page_shift = page_shift_of(cache->page_slots), a.max_pages = cache->max_pages;
+    a.hq = cfg->n_q_heads, a.hkv = cfg->n_kv_heads, a.head_dim = cfg->head_dim;
+    a.ws = static_cast<char*>(workspace);
+    a.lay = lay;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    const int threads = b->n_requests >= PAGE_PLAN_THREADS ? PAGE_PLAN_THREADS : (b->n_requests + 63) / 64 * 64;
+    DUO_LAUNCH(page_sum_kernel, dim3(1), dim3(threads), s, a);
+    const int longest = b->max_new > cache->max_pages ? b->max_new : cache->max_pages;
+    const int spread = longest > 8192 ? 16 : (longest + 511) / 512;
+    const int beyond = (cache->n_pages + 4095) / 4096 / spread + 1;
+    DUO_LAUNCH(page_fill_kernel, dim3(b->n_requests + beyond, spread), dim3(256), s, a);
+    return duo_internal_hip_ok(hipGetLastError(), "duo_page_plan");
+}
+
+extern "C" int duo_page_append(const duo_model_config* cfg, const duo_page_cache* cache, const duo_page_batch* b, int layer, const uint16_t* q,
+                               int64_t q_stride, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride, uint16_t* q_out,
+                               int64_t q_out_stride, void* hip_stream) {
+    if (const int rc = check_sizes(cfg, cache, b)) return rc;
+    if (layer < 0 || layer >= cfg->n_layers) return DUO_ERR_ARG;
+    if (!cache->k || !cache->v || !b->position || !b->slot || !b->status) return DUO_ERR_NULL;
+    if (off16(cache->k) || off16(cache->v) || off4(b->position) || off4(b->slot) || off4(b->status)) return DUO_ERR_ALIGN;
+    const int D = cfg->head_dim, qd = cfg->n_q_heads * D, kd = cfg->n_kv_heads * D;
+    if (const int rc = check_rows(q, q_stride, qd)) return rc;
+    if (const int rc = check_rows(k, k_stride, kd)) return rc;
+    if (const int rc = check_rows(v, v_stride, kd)) return rc;
+    if (const int rc = check_rows(q_out, q_out_stride, qd)) return rc;
+    if (q_out == q && q_out_stride != q_stride) return DUO_ERR_ARG;
+    PageAppendArgs a{};
+    a.q = q, a.k = k, a.v = v, a.q_out = q_out;
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
+    const size_t at = layer_elems(cfg, cache) * layer;
+    a.kc = cache->k + at, a.vc = cache->v + at;
+    a.position = b->position, a.slot = b->slot, a.status = b->status;
+    a.rows = b->max_rows, a.hq = cfg->n_q_heads, a.hkv = cfg->n_kv_heads, a.page_shift = page_shift_of(cache->page_slots), a.n_pages = cache->n_pages;
+    for (int d = 0; d < D / 2; ++d) a.turns[d] = pow((double)cfg->rope_theta, -2.0 * d / D) / (2.0 * M_PI);
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    const long long rope = (long long)b->max_rows * (cfg->n_q_heads + cfg->n_kv_heads) * (D / 16), vals = (long long)b->max_rows * cfg->n_kv_heads * (D / 8);
+    const dim3 gr((unsigned)((rope + 255) / 256)), gv((unsigned)((vals + 255) / 256));
+    if (D == 64) {
+        DUO_LAUNCH((page_rope_kernel<64>), gr, dim3(256), s, a);
+        DUO_LAUNCH((page_values_kernel<64>), gv, dim3(256), s, a);
+    } else {
+        DUO_LAUNCH((page_rope_kernel<128>), gr, dim3(256), s, a);
+        DUO_LAUNCH((page_values_kernel<128>), gv, dim3(256), s, a);
+    }
+    return duo_internal_hip_ok(hipGetLastError(), "duo_page_append");
+}
+
+extern "C" int duo_page_attention(const duo_model_config* cfg, const duo_page_cache* cache, const int32_t* block_table, const duo_page_batch* b, int layer,
+                                  const uint16_t* q, int64_t q_stride, uint16_t* out, int64_t out_stride, float scale, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
+    if (const int rc = check_sizes(cfg, cache, b)) return rc;
+    if (layer < 0 || layer >= cfg->n_layers || !(scale >= 0.f) || isinf(scale)) return DUO_ERR_ARG;
+    if (!cache->k || !cache->v || !block_table || !b->status) return DUO_ERR_NULL;
+    if (off16(cache->k) || off16(cache->v) || off4(block_table) || off4(b->status)) return DUO_ERR_ALIGN;
+    const int D = cfg->head_dim, qd = cfg->n_q_heads * D;
+    if (const int rc = check_rows(q, q_stride, qd)) return rc;
+    if (const int rc = check_rows(out, out_stride, qd)) return rc;
+    if (out == q) return DUO_ERR_ARG;
+    const PageLayout lay = layout_of(cfg, cache, b);
+    if (const int rc = check_workspace(lay, workspace, workspace_bytes)) return rc;
+    PageAttnArgs a{};
+    a.q = q, a.out = out, a.q_stride = q_stride, a.out_stride = out_stride;
+    const size_t at = layer_elems(cfg, cache) * layer;
+    a.kc = cache->k + at, a.vc = cache->v + at;
+    a.table = block_table, a.status = b->status;
+    char* const ws = static_cast<char*>(workspace);
+    a.ws = ws, a.info = lay.info, a.merge = lay.merge;
+    a.part_stream = reinterpret_cast<float*>(ws + lay.part_stream), a.part_tile = reinterpret_cast<float*>(ws + lay.part_tile);
+    a.stream_rows = lay.stream_rows;
+    a.requests = b->n_requests, a.hq = cfg->n_q_heads, a.hkv = cfg->n_kv_heads, a.page_shift = page_shift_of(cache->page_slots);
+    a.n_pages = cache->n_pages, a.max_pages = cache->max_pages, a.max_rows = b->max_rows, a.max_new = b->max_new;
+    a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    if (D == 64) launch_page_attention<64>(a, lay, s);
+    else launch_page_attention<128>(a, lay, s);
+    return duo_internal_hip_ok(hipGetLastError(), "duo_page_attention");
+}
+
+extern "C" int duo_page_commit(const duo_model_config* cfg, const duo_page_cache* cache, const int32_t* block_table, const duo_page_batch* b,
+                               const int32_t* records, int32_t* cached_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (const int rc = check_sizes(cfg, cache, b)) return rc;
+    if (!cache->k || !cache->v || !block_table || !b->status || !b->cached || !records || !cached_out) return DUO_ERR_NULL;
+    if (off16(cache->k) || off16(cache->v) || off4(block_table) || off4(b->status) || off4(b->cached) || off4(records) || off4(cached_out)) return DUO_ERR_ALIGN;
+    const PageLayout lay = layout_of(cfg, cache, b);
+    if (const int rc = check_workspace(lay, workspace, workspace_bytes)) return rc;
+    PageCommitArgs a{};
+    a.kc = cache->k, a.vc = cache->v, a.cached = b->cached, a.table = block_table, a.records = records, a.cached_out = cached_out, a.status = b->status;
+    a.requests = b->n_requests, a.layers = cfg->n_layers, a.hkv = cfg->n_kv_heads, a.page_shift = page_shift_of(cache->page_slots), a.n_pages = cache->n_pages;
+    a.max_pages = cache->max_pages, a.max_new = b->max_new, a.hq = cfg->n_q_heads, a.head_dim = cfg->head_dim, a.max_rows = b->max_rows;
+    a.ws = static_cast<const char*>(workspace), a.info = lay.info;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    const dim3 grid(b->n_requests, cfg->n_layers, cfg->n_kv_heads);
+    if (cfg->head_dim == 64) DUO_LAUNCH((page_commit_kernel<64>), grid, dim3(128), s, a);
+    else DUO_LAUNCH((page_commit_kernel<128>), grid, dim3(128), s, a);
+    return duo_internal_hip_ok(hipGetLastError(), "duo_page_commit");
+}

@@ -1,0 +1,82 @@
+// Sizes and schedules of the paged-cache calls: plain arithmetic without a word of HIP but for the qualifiers of what a kernel calls too, so
+// that a program without a GPU can evaluate them.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+// The attention of a step is cut into items, one workgroup for each of them and each kv head.  An item is a tile of query rows (row = token
+// of the request * group + query head of the group) and a range of 32-key blocks.
+//   Streamed: up to PAGE_STREAM_ROWS rows, the whole request in one tile.  The cache is read once and bounds the time, so the waves of a
+//     workgroup take different blocks.
+//   Tiled: more rows, tiles of PAGE_TILE_ROWS.  The matrix units bound the time, so the waves take different rows and share the blocks in LDS.
+constexpr int PAGE_STREAM_ROWS = 64;
+constexpr int PAGE_TILE_ROWS = 256;
+// Workgroups that the key ranges are cut for (fewer rows and requests than that are split over the keys), and the shortest ranges.
+constexpr int PAGE_STREAM_TARGET = 1024, PAGE_STREAM_MIN_BLOCKS = 8;
+constexpr int PAGE_TILE_TARGET = 512, PAGE_TILE_MIN_BLOCKS = 16;
+
+// Limits that keep every sum of a plan inside 32 bits: 4096 requests of 2^18 rows, 2^18 pages or 2^18 blocks each.
+constexpr int PAGE_MAX_REQUESTS = 4096, PAGE_MAX_ROWS = 1 << 18, PAGE_MAX_SLOTS = 1 << 23;
+
+struct PageWork {       // what a request asks of the attention, and how it is cut
+    int blocks;         // 32-key blocks of all its slots
+    int tiles;          // tiles of query rows; 0: nothing to do
+    bool streamed;
+};
+__host__ __device__ __forceinline__ PageWork page_work(int cached, int rows_new, int group) {
+    PageWork w;
+    w.blocks = (cached + rows_new + 31) / 32;
+    w.streamed = rows_new * group <= PAGE_STREAM_ROWS;
+    w.tiles = rows_new == 0 ? 0 : w.streamed ? 1 : (rows_new * group + PAGE_TILE_ROWS - 1) / PAGE_TILE_ROWS;
+    return w;
+}
+// Longest key range, in blocks, for `work` = sum of tiles * blocks over the requests of a kind: work / range is then at most target / heads.
+__host__ __device__ __forceinline__ int page_range(long long work, int heads, int target, int least) {
+    const long long r = (work * heads + target - 1) / target;
+    return r < least ? least : (int)r;
+}
+// A tile that sees `blocks` blocks is cut into at most `chunks` ranges of this length.
+__host__ __device__ __forceinline__ int page_chunk_blocks(int blocks, int chunks) { return (blocks + chunks - 1) / chunks; }
+// Blocks that the rows [first, first + count) of a request see.
+__host__ __device__ __forceinline__ int page_tile_blocks(int cached, int first, int count, int group) { return (cached + (first + count - 1) / group) / 32 + 1; }
+
+// Where things lie in the workspace, and how many of each there can be whatever the lengths are.
+//   items of a kind: sum of tiles * ceil(blocks / range) <= work / range + sum of tiles <= target / heads + tiles
+//   ranges of requests that are cut: ceil(blocks / range) <= 2 blocks / range there, so at most 2 target / heads of them
+struct PageLayout {
+    int stream_items, tile_items, stream_parts, tile_parts, merges;
+    int stream_rows;  // rows kept per streamed partial result
+    size_t info, stream, tile, merge, part_stream, part_tile, total;
+};
+constexpr int PAGE_HEADER_INTS = 64, PAGE_INFO_INTS = 16, PAGE_ITEM_INTS = 16, PAGE_MERGE_INTS = 8;
+
+inline PageLayout page_layout(int requests, int max_rows, int max_new, int max_blocks, int hq, int hkv, int D) {
+    const int group = hq / hkv;
+    const bool tiles_possible = (long long)max_new * group > PAGE_STREAM_ROWS;
+    PageLayout l;
+    l.stream_items = PAGE_STREAM_TARGET / hkv + requests;
+    l.stream_parts = max_blocks > PAGE_STREAM_MIN_BLOCKS ? 2 * PAGE_STREAM_TARGET / hkv : 0;
+    // a tiled request has more than PAGE_STREAM_ROWS rows
+    const long long all = (long long)max_rows * group;
+    const long long tiled_requests = all / (PAGE_STREAM_ROWS + 1) < requests ? all / (PAGE_STREAM_ROWS + 1) : requests;
+    l.tile_items = tiles_possible ? (int)(PAGE_TILE_TARGET / hkv + all / PAGE_TILE_ROWS + tiled_requests) : 0;
+    l.tile_parts = tiles_possible && max_blocks > PAGE_TILE_MIN_BLOCKS ? 2 * PAGE_TILE_TARGET / hkv : 0;
+    l.merges = (l.stream_parts + l.tile_parts) / 2;  // two ranges at least
+    const long long rows = (long long)max_new * group;
+    l.stream_rows = rows >= PAGE_STREAM_ROWS ? PAGE_STREAM_ROWS : (int)((rows + 15) / 16 * 16);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    take(PAGE_HEADER_INTS * 4);
+    l.info = take((size_t)requests * PAGE_INFO_INTS * 4);
+    l.stream = take((size_t)l.stream_items * PAGE_ITEM_INTS * 4);
+    l.tile = take((size_t)l.tile_items * PAGE_ITEM_INTS * 4);
+    l.merge = take((size_t)l.merges * PAGE_MERGE_INTS * 4);
+    l.part_stream = take((size_t)l.stream_parts * hkv * l.stream_rows * (D + 4) * 4);
+    l.part_tile = take((size_t)l.tile_parts * hkv * PAGE_TILE_ROWS * (D + 4) * 4);
+    l.total = off;
+    return l;
+}
