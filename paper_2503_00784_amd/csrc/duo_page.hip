@@ -64,7 +64,7 @@ void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStre
     if (lay.tile_items > 0) {
         PageAttnArgs tl = a;
         tl.items = lay.tile;
-        DUO_LAUNCH((page_tile_kernel<D>), dim3(lay.tile_items * a.hkv), dim3(512), s, tl);
+        DUO_LAUNCH((page_tile_kernel<D>), dim3(lay.tile_items * a.hkv), dim3(256), s, tl);
     }
     if (lay.merges > 0)
         DUO_LAUNCH((page_merge_kernel<D>), dim3(lay.merges * a.hkv, lay.tile_parts > 0 ? 16 : lay.stream_rows / 4), dim3(256), s, a);

@@ -25,7 +25,7 @@ struct PageAttnArgs {
     float scale_log2;
 };
 
-constexpr float PAGE_LAG = 8.f;  // log2 of the largest softmax weight: the reference stays this far behind at most
+constexpr float PAGE_LAG = 8.f, PAGE_MOST = 256.f;  // the largest softmax weight and its log2: so far the reference may stay behind
 
 // What a row sees: slots below `before`, and slots from `lo` to `hi`.
 struct PageSight {
@@ -58,9 +58,11 @@ __device__ __forceinline__ PageItem page_item(const PageItem* p) {  // the same 
 }
 // 16 bytes per lane from global memory to LDS, lane after lane from `lds` on.  In assembly because of the waits: a wave that both requests
 // and reads LDS would otherwise wait for all of its requests in front of every read.  The wave waits for them itself (page_stage_landed).
-__device__ __forceinline__ void page_load_lds(const u16* src, const void* lds) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)lds);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(at) : "memory", "m0");
+__device__ __forceinline__ void page_load_lds(const u16* src, uint32_t lane_bytes, uint32_t lds) {  // src and lds the same in all lanes
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_bytes), "s"(src), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
 }
 // All but the newest N of this wave's vector memory requests and all of its LDS reads have come back; then the workgroup's barrier.  Nothing
 // moves across.
@@ -338,9 +340,10 @@ __global__ __launch_bounds__(256) void page_stream_kernel(PageAttnArgs a) {
 
 // ---- many rows: the matrix units bound the time
 //
-// Eight waves of 32 rows; a block of 32 keys is put in LDS once for all of them (16-byte loads from global memory to LDS, three stages of two
-// blocks, one barrier a stage).  32 x 32 x 16 products: the tiles' lanes are picked from LDS so that a lane's scores are eight
-// consecutive keys twice over, which is the operand of the second product.
+// Four waves of 32 rows; keys and values of two blocks (a stage) at a time are put in LDS for all of them by 16-byte loads from global memory to
+// LDS.  32 x 32 x 16 products: the tiles' lanes are picked from LDS so that a lane's scores are eight consecutive keys twice over,
+// which is the operand of the second product.  The scores of a stage are formed while the weights of the one before are, so K runs a stage
+// ahead of V; one barrier a stage.
 __device__ __forceinline__ f32x16 mfma32(elem8 a, elem8 b, f32x16 c) {
     // D[32x32] += A[32x16] * B[16x32]; lane l supplies A[l%32][8*(l/32) .. +8] and B[8*(l/32) .. +8][l%32]; register i of lane l is
     // D[8*(i/4) + 4*(l/32) + i%4][l%32].
@@ -356,149 +359,169 @@ __device__ __forceinline__ float lane_halves_max(float x) {
 }
 
 template <int D>
-__global__ __launch_bounds__(512) void page_tile_kernel(PageAttnArgs a) {
-    constexpr int KS = D / 32, DT = D / 16, C32 = D / 32, NW = 8;
-    constexpr int TILES = 2 * KS + DT;   // 1 KiB tiles of a block: keys, then values
-    constexpr int BPS = 2, NBUF = 3;     // blocks a stage, stages
-    constexpr int PER_WAVE = BPS * TILES / NW;
-    static_assert(BPS * TILES % NW == 0 && TILES % PER_WAVE == 0, "every wave moves the same number of tiles of one block");
-    __shared__ u32x4 lds_kv[NBUF][BPS * TILES * 64];
+__global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
+    constexpr int KS = D / 32, DT = D / 16, C32 = D / 32, NW = 4;
+    constexpr int KT = 2 * KS, BPS = 2;            // 1 KiB tiles of a block's keys (and DT of its values), blocks a stage
+    constexpr int KPW = BPS * KT / NW, VPW = BPS * DT / NW;  // tiles that a wave moves, of one block: waves 0 and 1 the first, 2 and 3 the second
+    static_assert(NW * 32 == PAGE_TILE_ROWS && KT == DT && NW == 2 * BPS, "a workgroup takes a tile, two waves move a block");
+    __shared__ u32x4 lds_k[2][BPS * KT * 64], lds_v[2][BPS * DT * 64];
     const int index = blockIdx.x / a.hkv, hk = blockIdx.x - index * a.hkv;
+    const PageItem it = page_item(reinterpret_cast<const PageItem*>(a.ws + a.items) + index);  // of no meaning behind the last
     const PageHeader* hdr = reinterpret_cast<const PageHeader*>(a.ws);
     if (!page_plan_is(*hdr, a.requests, a.hq, a.hkv, D, a.page_shift, a.max_pages, a.max_rows, a.max_new)) return;  // reported by the other kernel
     if (index >= hdr->tile_items) return;
-    const PageItem it = page_item(reinterpret_cast<const PageItem*>(a.ws + a.items) + index);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int col = lane & 31, half = lane >> 5;
     const int group = a.hq / a.hkv;
 
-    const int r = wave * 32 + col;  // of the tile
-    const bool valid = r < it.count;
-    const int pair = it.first + (valid ? r : 0);
-    const int token = pair / group, gq = pair - token * group;
-    const PageSight sight = page_sight(it, token, valid);
-    elem8 qf[2 * KS];
-    {
-        const u16* qp = a.q + (size_t)(it.row0 + token) * a.q_stride + (hk * group + gq) * D + half * 8;
-#pragma unroll
-        for (int s = 0; s < 2 * KS; ++s) {
-            Frag8 f;
-            f.q = valid ? *reinterpret_cast<const u32x4*>(qp + s * 16) : u32x4{0u, 0u, 0u, 0u};
-            qf[s] = f.v;
-        }
-    }
-    // slots below are seen by all of the wave's rows; the last slot that any of them sees
-    const int wave_first = (it.first + wave * 32) / group;
-    const int rows_here = min(32, it.count - wave * 32);
-    const int sees_all = it.cached + min(wave_first + 1, it.trunk);
-    const int sees_last = rows_here > 0 ? it.cached + (it.first + wave * 32 + rows_here - 1) / group : -1;
-
+    // The wave moves half a block of keys and half a block of values a stage.  Stage st holds the values of blocks 2 st and 2 st + 1 of the range and the
+    // keys of 2 st + 1 and 2 st + 2; stage -1 the keys of block 0.  Blocks behind the range repeat its last one and are not used.
     const int32_t* line = a.table + (size_t)it.request * a.max_pages;
     const int shift = a.page_shift - 5;
     const int nst = (it.blocks + BPS - 1) / BPS;
-    const int my_block = wave * PER_WAVE / TILES;  // of the stage: the block that this wave moves tiles of
-    const int my_tile = wave * PER_WAVE % TILES;
-    int ids = 0;
-    auto fetch_ids = [&](int st) {  // pages of this wave's block in stages st .. st + 63
-        const int b = min(it.block0 + min((st + lane) * BPS + my_block, it.blocks - 1), it.last_block);
-        const int id = line[b >> shift];
+    const int my_block = wave >> 1, my_tile = (wave & 1) * KPW;
+    const uint32_t lds_k_mine = lds_address(lds_k) + (my_block * KT + my_tile) * 1024, lds_v_mine = lds_address(lds_v) + (my_block * DT + my_tile) * 1024;
+    auto fetch_id = [&](int b) {  // page of block b of the range, b differs from lane to lane
+        const int id = line[min(it.block0 + min(b, it.blocks - 1), it.last_block) >> shift];
         const bool fine = (unsigned)id < (unsigned)a.n_pages;
         if (!fine) atomicOr(a.status, DUO_PAGE_BAD_PAGE);
-        ids = fine ? id : 0;
+        return fine ? id : 0;
     };
-    auto issue = [&](int st) {  // blocks behind the range repeat its last one and are not used
-        if ((st & 63) == 0) fetch_ids(st);
-        const int b = it.block0 + min(st * BPS + my_block, it.blocks - 1);
-        const int id = __builtin_amdgcn_readlane(ids, st & 63);
-        const size_t at = ((((size_t)id * a.hkv + hk) << a.page_shift) + ((b & ((1 << shift) - 1)) << 5)) * D + lane * 8;
-        u32x4* dst = lds_kv[st % NBUF] + my_block * TILES * 64;
-#pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) {
-            const int j = my_tile + i;
-            const u16* src = j < 2 * KS ? a.kc + at + j * 512 : a.vc + at + (j - 2 * KS) * 512;
-            page_load_lds(src, dst + j * 64);
+    auto place = [&](int id, int b) {  // of this wave's tiles of block b
+        const int in_page = (it.block0 + min(b, it.blocks - 1)) & ((1 << shift) - 1);
+        return ((((size_t)id * a.hkv + hk) << a.page_shift) + (in_page << 5)) * D + my_tile * 512;
+    };
+    int ids_k = 0, ids_v = 0;  // pages of the wave's blocks in stages st .. st + 63
+    auto request = [&](int st) {
+        if ((st & 63) == 0) {
+            ids_k = fetch_id((st + lane) * BPS + my_block + 1);
+            ids_v = fetch_id((st + lane) * BPS + my_block);
         }
+        const u16* k = a.kc + place(__builtin_amdgcn_readlane(ids_k, st & 63), st * BPS + my_block + 1);
+        const u16* v = a.vc + place(__builtin_amdgcn_readlane(ids_v, st & 63), st * BPS + my_block);
+#pragma unroll
+        for (int i = 0; i < VPW; ++i) page_load_lds(v + i * 512, lane * 16, lds_v_mine + (st & 1) * (BPS * DT * 1024) + i * 1024);
+#pragma unroll
+        for (int i = 0; i < KPW; ++i) page_load_lds(k + i * 512, lane * 16, lds_k_mine + (st & 1) * (BPS * KT * 1024) + i * 1024);
     };
+    if (nst > 0) {
+        {
+            const u16* k = a.kc + place(__builtin_amdgcn_readfirstlane(fetch_id(0)), 0);
+            const int half_mine = (my_block * (KPW / 2)) ;  // block 0 is shared out among all four waves
+#pragma unroll
+            for (int i = 0; i < KPW / 2; ++i)
+                page_load_lds(k + (half_mine + i) * 512, lane * 16, lds_address(lds_k) + ((BPS + 1) * KT + my_tile + half_mine + i) * 1024);
+        }
+        request(0);
+    }
+
+    const int r = wave * 32 + col;  // of the tile
+    const bool valid = r < it.count;
+    const int pair = it.first + (valid ? r : 0);  // rows behind the tile's last take the first's queries and see nothing
+    const int token = pair / group, gq = pair - token * group;
+    const PageSight sight = page_sight(it, token, valid);
+    elem8 qf[KT];
+    {
+        const u16* qp = a.q + (size_t)(it.row0 + token) * a.q_stride + (hk * group + gq) * D + half * 8;
+#pragma unroll
+        for (int s = 0; s < KT; ++s) {
+            Frag8 f;
+            f.q = *reinterpret_cast<const u32x4*>(qp + s * 16);
+            qf[s] = f.v;
+        }
+    }
+    // the last slot that any of the wave's rows sees
+    const int rows_here = min(32, it.count - wave * 32);
+    const int sees_last = rows_here > 0 ? it.cached + (it.first + wave * 32 + rows_here - 1) / group : -1;
 
     f32x16 o[C32];
     float m = -INFINITY, l = 0.f;
+    auto zero = [] {
+        f32x16 z;
 #pragma unroll
-    for (int d = 0; d < C32; ++d)
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+        return z;
+    };
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-
-    auto use_block = [&](const u32x4* buf, int kb) {
-        const u32x4* kt = buf + ((col >> 4) * KS * 64 + half * 16 + (col & 15));
-        const u32x4* vt = buf + 2 * KS * 64 + ((col >> 4) * 64 + half * 16 + (col & 15));
-        f32x16 s;
+    for (int d = 0; d < C32; ++d) o[d] = zero();
+    const int frag_k = (col >> 4) * KS * 64 + half * 16 + (col & 15), frag_v = (col >> 4) * 64 + half * 16 + (col & 15);
+    auto value_frag = [&](int st, int z, int d, int jj) {
+        Frag8 f;
+        f.q = lds_v[st & 1][z * DT * 64 + frag_v + 2 * d * 64 + 2 * jj * 16];
+        return f.v;
+    };
+    auto take_keys = [&](elem8 (&f)[KT], int st, int z) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 2 * KS; ++j) {
-            Frag8 f;
-            f.q = kt[(j >> 1) * 64 + (j & 1) * 32];
-            s = mfma32(f.v, qf[j], s);
+        for (int j = 0; j < KT; ++j) {
+            Frag8 x;
+            x.q = lds_k[st & 1][z * KT * 64 + frag_k + (j >> 1) * 64 + (j & 1) * 32];
+            f[j] = x.v;
         }
-        const bool masked = kb + 32 > sees_all;
-        if (masked) {
+    };
+    auto take_values = [&](elem8 (&f)[C32][2], int st, int z) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = sight(kb + 8 * (half + 2 * ((i >> 2) & 1)) + 4 * (i >> 3) + (i & 3)) ? s[i] : -INFINITY;
-        }
-        float top = s[0];
+        for (int d = 0; d < C32; ++d)
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        top *= a.scale_log2;
-        if (__ballot(top > m + PAGE_LAG)) {
-            const float m_new = fmaxf(m, lane_halves_max(top));
-            const float alpha = exp2_raw(m - (m_new == -INFINITY ? 0.f : m_new));
+            for (int jj = 0; jj < 2; ++jj) f[d][jj] = value_frag(st, z, d, jj);
+    };
+    auto scores = [&](const elem8 (&f)[KT]) {
+        f32x16 s = zero();
+#pragma unroll
+        for (int j = 0; j < KT; ++j) s = mfma32(f[j], qf[j], s);
+        return s;
+    };
+    auto add_values = [&](const elem8 (&f)[C32][2], const Frag8 (&p)[2]) {
+#pragma unroll
+        for (int d = 0; d < C32; ++d)
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) o[d] = mfma32(f[d][jj], p[jj].v, o[d]);
+    };
+    // The softmax weights of a block, as operands; l takes their sum.  The row's reference stays where it is while a lane's weights sum to no more
+    // than 2^8, so none of them is larger: no maximum is looked for.  It moves, to the maximum, when they sum to more, and at the first
+    // block (m = -inf makes infinities or NaN of them).
+    auto weigh = [&](const f32x16& s, Frag8 (&p)[2], auto order) {
+        auto with = [&](float ref) {
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 4 * jj + 8 * (e >> 1) + 2 * (e & 1);
+                    const float w0 = exp2_raw(fmaf(s[i], a.scale_log2, -ref)), w1 = exp2_raw(fmaf(s[i + 1], a.scale_log2, -ref));
+                    sum[0] += w0;
+                    sum[1] += w1;
+                    p[jj].q[e] = pack_elem2(w0, w1);
+                }
+            return sum[0] + sum[1];
+        };
+        float sum = with(m);
+        order();
+        if (__builtin_expect(__ballot(!(sum <= PAGE_MOST)) != 0, 0)) {
+            asm volatile("");  // a branch, rather than both sides of it every time
+            float top = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+            const float m_new = fmaxf(m, lane_halves_max(top * a.scale_log2)), ref = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = exp2_raw(m - ref);
             m = m_new;
             l *= alpha;
 #pragma unroll
             for (int d = 0; d < C32; ++d) o[d] = o[d] * alpha;
+            sum = with(ref);
         }
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[i] = exp2_raw(fmaf(s[i], a.scale_log2, -ref));
-            l += s[i];
-        }
-        Frag8 p[2];
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 4 * jj + 8 * (e >> 1) + 2 * (e & 1);
-                p[jj].q[e] = pack_elem2(s[i], s[i + 1]);
-            }
-        if (!masked) {
-#pragma unroll
-            for (int d = 0; d < C32; ++d)
-#pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {
-                    Frag8 f;
-                    f.q = vt[2 * d * 64 + 2 * jj * 16];
-                    o[d] = mfma32(f.v, p[jj].v, o[d]);
-                }
-            return;
-        }
+        l += sum;
+    };
+    // The values of a block that some rows do not see whole.
+    auto add_masked = [&](int st, int z, int kb, const Frag8 (&p)[2]) {
+        auto kept = [&](int d, int jj) { return keep_keys(value_frag(st, z, d, jj), it.slots - kb - 8 * (2 * jj + half)); };  // slots behind the last may hold anything
         uint32_t odd = 0;
 #pragma unroll
-        for (int d = 0; d < C32; ++d)
-#pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
-                Frag8 f;
-                f.q = vt[2 * d * 64 + 2 * jj * 16];
-                odd |= not_finite(keep_keys(f.v, it.slots - kb - 8 * (2 * jj + half)));  // slots behind the last may hold anything
-            }
-        if (!__any((odd & NOT_FINITE) != 0)) {
+        for (int d = 0; d < C32; ++d) odd |= not_finite(kept(d, 0)) | not_finite(kept(d, 1));
+        if (__builtin_expect(!__any((odd & NOT_FINITE) != 0), 1)) {
 #pragma unroll
             for (int d = 0; d < C32; ++d)
 #pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {
-                    Frag8 f;
-                    f.q = vt[2 * d * 64 + 2 * jj * 16];
-                    o[d] = mfma32(keep_keys(f.v, it.slots - kb - 8 * (2 * jj + half)), p[jj].v, o[d]);
-                }
+                for (int jj = 0; jj < 2; ++jj) o[d] = mfma32(kept(d, jj), p[jj].v, o[d]);
             return;
         }
         const int keys = min(32, it.slots - kb);  // key by key, each added only where it is seen: 0 * inf is not 0
@@ -507,13 +530,9 @@ __global__ __launch_bounds__(512) void page_tile_kernel(PageAttnArgs a) {
 #pragma unroll 1
             for (int key = 0; key < keys; ++key) {
                 const int jj = key >> 4;
-                Frag8 f, w;
-                f.q = vt[2 * d * 64 + 2 * jj * 16];
+                Frag8 w;
                 w.q = jj ? p[1].q : p[0].q;
-                f32x16 add;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) add[i] = 0.f;
-                add = mfma32(one_key(f.v, key, half == ((key >> 3) & 1)), w.v, add);
+                const f32x16 add = mfma32(one_key(value_frag(st, z, d, jj), key, half == ((key >> 3) & 1)), w.v, zero());
                 const bool seen = sight(kb + key);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] += seen ? add[i] : 0.f;
@@ -522,16 +541,48 @@ __global__ __launch_bounds__(512) void page_tile_kernel(PageAttnArgs a) {
     };
 
     if (nst > 0) {
-        issue(0);
-        issue(1);
-        for (int st = 0; st < nst; ++st) {
-            page_stage_landed<PER_WAVE>();  // stage st is there (what may be in flight is stage st + 1), stage st - 1 drained
-            issue(st + 2);
+        // Stages that every row of the workgroup sees whole come first.
+        const int all_see = it.cached + min(it.first / group + 1, it.trunk) - it.block0 * 32;
+        const int whole = min(max(all_see, 0) / (32 * BPS), it.blocks / BPS);
+        page_stage_landed<KPW + VPW>();  // the keys of block 0
+        elem8 kf[KT], vf[C32][2];
+        Frag8 p[2];
+        take_keys(kf, -1, 1);
+        f32x16 s0 = scores(kf), s1;
+        int st = 0;
+#pragma unroll 1
+        for (; st < whole; ++st) {
+            page_stage_landed<0>();  // stage st is there, stage st - 1 drained
+            request(st + 1);
+            take_keys(kf, st, 0);
+            take_values(vf, st, 0);
+            s1 = scores(kf);
+            weigh(s0, p, [] {});
+            take_keys(kf, st, 1);
+            add_values(vf, p);
+            take_values(vf, st, 1);
+            s0 = scores(kf);
+            weigh(s1, p, [] {});
+            add_values(vf, p);
+        }
+        auto masked = [&](f32x16& s, int b) {  // block b of the range, its scores s
+            const int kb = (it.block0 + b) * 32;
+            if (b >= it.blocks || kb > sees_last) return;
 #pragma unroll
-            for (int z = 0; z < BPS; ++z) {
-                const int b = st * BPS + z, kb = (it.block0 + b) * 32;
-                if (b < it.blocks && kb <= sees_last) use_block(lds_kv[st % NBUF] + z * TILES * 64, kb);
-            }
+            for (int i = 0; i < 16; ++i) s[i] = sight(kb + 8 * (half + 2 * ((i >> 2) & 1)) + 4 * (i >> 3) + (i & 3)) ? s[i] : -INFINITY;
+            weigh(s, p, [] {});
+            add_masked(st, b & 1, kb, p);
+        };
+#pragma unroll 1
+        for (; st < nst; ++st) {
+            page_stage_landed<0>();
+            request(st + 1);
+            masked(s0, st * BPS);
+            take_keys(kf, st, 0);
+            s1 = scores(kf);
+            masked(s1, st * BPS + 1);
+            take_keys(kf, st, 1);
+            s0 = scores(kf);
         }
         page_stage_landed<0>();  // nothing is in flight to LDS when the workgroup ends
     }

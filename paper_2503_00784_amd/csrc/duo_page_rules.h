@@ -10,7 +10,7 @@
 //     workgroup take different blocks.
 //   Tiled: more rows, tiles of PAGE_TILE_ROWS.  The matrix units bound the time, so the waves take different rows and share the blocks in LDS.
 constexpr int PAGE_STREAM_ROWS = 64;
-constexpr int PAGE_TILE_ROWS = 256;
+constexpr int PAGE_TILE_ROWS = 128;
 // Workgroups that the key ranges are cut for (fewer rows and requests than that are split over the keys), and the shortest ranges.
 constexpr int PAGE_STREAM_TARGET = 1024, PAGE_STREAM_MIN_BLOCKS = 8;
 constexpr int PAGE_TILE_TARGET = 512, PAGE_TILE_MIN_BLOCKS = 16;

@@ -12,7 +12,7 @@ from paper_2503_00784_amd import binding as B
 from paper_2503_00784_amd import inputs
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-TILE_ROWS = 256
+TILE_ROWS = 128
 
 
 @functools.lru_cache(maxsize=None)
