@@ -36,8 +36,10 @@ struct __align__(16) PageItem {  // one workgroup per item and kv head
 };
 static_assert(sizeof(PageItem) == PAGE_ITEM_INTS * 4, "the place of an item");
 
-struct __align__(16) PageMerge {  // a tile whose keys were cut
-    int32_t row0, first, count, part0, parts, streamed, pad[2];
+struct __align__(16) PageMerge {  // some rows of a tile whose keys were cut
+    int32_t row0, first, count;  // the request's first row; pairs first .. first + count - 1
+    int32_t part0, parts;        // its tile's partial results
+    int32_t in_tile, streamed, pad;
 };
 static_assert(sizeof(PageMerge) == PAGE_MERGE_INTS * 4, "the place of a merge");
 
@@ -151,7 +153,7 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
         q.chunks = (blocks + range - 1) / range;
         const int items = q.tiles * q.chunks;
         cut[q.streamed ? ITEM_S : ITEM_T] += items;
-        if (q.chunks > 1) cut[q.streamed ? PART_S : PART_T] += items, cut[MERGE] += q.tiles;
+        if (q.chunks > 1) cut[q.streamed ? PART_S : PART_T] += items, cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
     }
     int cuts[CUTS];
     block_scan(cut, cuts, scan);
@@ -189,7 +191,7 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
         if (q.chunks > 1) {
             int& part = cut[q.streamed ? PART_S : PART_T];
             q.part0 = part, q.merge0 = cut[MERGE];
-            part += items, cut[MERGE] += q.tiles;
+            part += items, cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
         }
         info[r] = q;
         a.held_out[r] = q.need;
@@ -274,11 +276,19 @@ __global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
         it.last_block = (it.slots - 1) >> 5;
         it.pad[0] = it.pad[1] = it.pad[2] = it.pad[3] = 0;
         out[i] = it;
-        if (p.chunks > 1 && chunk == 0) {
+    }
+    if (p.chunks > 1) {
+        const int rows = page_merge_rows(p.chunks), entries = page_merge_entries(pairs, p.chunks);
+        PageMerge* const merge = reinterpret_cast<PageMerge*>(a.ws + a.lay.merge) + p.merge0;
+        for (int i = t0; i < entries; i += step) {
+            const int first = i * rows, tile = p.streamed ? 0 : first / PAGE_TILE_ROWS, tile_first = tile * PAGE_TILE_ROWS;
+            const int count = p.streamed ? pairs : min(PAGE_TILE_ROWS, pairs - tile_first);
+            const int blocks = page_tile_blocks(p.cached, tile_first, count, group), length = page_chunk_blocks(blocks, p.chunks);
             PageMerge m;
-            m.row0 = p.row0, m.first = first, m.count = count, m.part0 = p.part0 + tile * p.chunks, m.parts = (blocks + length - 1) / length;
-            m.streamed = p.streamed, m.pad[0] = m.pad[1] = 0;
-            reinterpret_cast<PageMerge*>(a.ws + a.lay.merge)[p.merge0 + tile] = m;
+            m.row0 = p.row0, m.first = first, m.count = min(rows, pairs - first);
+            m.part0 = p.part0 + tile * p.chunks, m.parts = (blocks + length - 1) / length;
+            m.in_tile = first - tile_first, m.streamed = p.streamed, m.pad = 0;
+            merge[i] = m;
         }
     }
 }

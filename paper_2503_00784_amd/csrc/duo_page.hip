@@ -54,20 +54,15 @@ size_t layer_elems(const duo_model_config* cfg, const duo_page_cache* c) { retur
 
 template <int D>
 void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStream_t s) {
-    PageAttnArgs st = a;
-    st.items = lay.stream;
-    const dim3 grid(lay.stream_items * a.hkv);
-    if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D, 1>), grid, dim3(256), s, st);
-    else if (lay.stream_rows <= 32) DUO_LAUNCH((page_stream_kernel<D, 2>), grid, dim3(256), s, st);
-    else if (lay.stream_rows <= 48) DUO_LAUNCH((page_stream_kernel<D, 3>), grid, dim3(256), s, st);
-    else DUO_LAUNCH((page_stream_kernel<D, 4>), grid, dim3(256), s, st);
-    if (lay.tile_items > 0) {
-        PageAttnArgs tl = a;
-        tl.items = lay.tile;
-        DUO_LAUNCH((page_tile_kernel<D>), dim3(lay.tile_items * a.hkv), dim3(256), s, tl);
+    const unsigned few = lay.stream_items * a.hkv;  // more workgroups than the plan has items end at once
+    if (lay.tile_items > 0) DUO_LAUNCH((page_mixed_kernel<D>), dim3(lay.tile_items * a.hkv + few), dim3(256), s, a);
+    else if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D>), dim3(few), dim3(256), s, a);
+    else if (lay.stream_rows <= 32) DUO_LAUNCH((page_team_kernel<D, 1>), dim3(few), dim3(128), s, a);
+    else DUO_LAUNCH((page_team_kernel<D, 2>), dim3(few), dim3(256), s, a);
+    if (lay.merges > 0) {
+        const long long units = (long long)lay.merges * a.hkv;
+        DUO_LAUNCH((page_merge_kernel<D>), dim3(units < 4096 ? (int)units : 4096), dim3(256), s, a);
     }
-    if (lay.merges > 0)
-        DUO_LAUNCH((page_merge_kernel<D>), dim3(lay.merges * a.hkv, lay.tile_parts > 0 ? 16 : lay.stream_rows / 4), dim3(256), s, a);
 }
 
 }  // namespace
@@ -167,9 +162,9 @@ extern "C" int duo_page_attention(const duo_model_config* cfg, const duo_page_ca
     a.kc = cache->k + at, a.vc = cache->v + at;
     a.table = block_table, a.status = b->status;
     char* const ws = static_cast<char*>(workspace);
-    a.ws = ws, a.info = lay.info, a.merge = lay.merge;
+    a.ws = ws, a.stream = lay.stream, a.tile = lay.tile, a.merge = lay.merge;
     a.part_stream = reinterpret_cast<float*>(ws + lay.part_stream), a.part_tile = reinterpret_cast<float*>(ws + lay.part_tile);
-    a.stream_rows = lay.stream_rows;
+    a.stream_rows = lay.stream_rows, a.tile_items = lay.tile_items;
     a.requests = b->n_requests, a.hq = cfg->n_q_heads, a.hkv = cfg->n_kv_heads, a.page_shift = page_shift_of(cache->page_slots);
     a.n_pages = cache->n_pages, a.max_pages = cache->max_pages, a.max_rows = b->max_rows, a.max_new = b->max_new;
     a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;

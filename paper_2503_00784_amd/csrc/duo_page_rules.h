@@ -37,6 +37,11 @@ __host__ __device__ __forceinline__ int page_range(long long work, int heads, in
 }
 // A tile that sees `blocks` blocks is cut into at most `chunks` ranges of this length.
 __host__ __device__ __forceinline__ int page_chunk_blocks(int blocks, int chunks) { return (blocks + chunks - 1) / chunks; }
+// Joining the ranges of a tile: a workgroup and head takes this many rows, fewer where a row has many ranges.
+constexpr int PAGE_MERGE_RANGES = 8;
+__host__ __device__ __forceinline__ int page_merge_rows(int chunks) { return chunks > PAGE_MERGE_RANGES ? 1 : 16; }
+__host__ __device__ __forceinline__ int page_merge_entries(int pairs, int chunks) { return (pairs + page_merge_rows(chunks) - 1) / page_merge_rows(chunks); }
+static_assert(PAGE_TILE_ROWS % 16 == 0 && PAGE_STREAM_ROWS % 16 == 0, "an entry's rows are of one tile");
 // Blocks that the rows [first, first + count) of a request see.
 __host__ __device__ __forceinline__ int page_tile_blocks(int cached, int first, int count, int group) { return (cached + (first + count - 1) / group) / 32 + 1; }
 
@@ -61,9 +66,10 @@ inline PageLayout page_layout(int requests, int max_rows, int max_new, int max_b
     const long long tiled_requests = all / (PAGE_STREAM_ROWS + 1) < requests ? all / (PAGE_STREAM_ROWS + 1) : requests;
     l.tile_items = tiles_possible ? (int)(PAGE_TILE_TARGET / hkv + all / PAGE_TILE_ROWS + tiled_requests) : 0;
     l.tile_parts = tiles_possible && max_blocks > PAGE_TILE_MIN_BLOCKS ? 2 * PAGE_TILE_TARGET / hkv : 0;
-    l.merges = (l.stream_parts + l.tile_parts) / 2;  // two ranges at least
     const long long rows = (long long)max_new * group;
     l.stream_rows = rows >= PAGE_STREAM_ROWS ? PAGE_STREAM_ROWS : (int)((rows + 15) / 16 * 16);
+    // a tile of up to R rows has 2 ranges or more and R / 16 entries at most, or 9 ranges or more and R entries: R / 8 entries a range at most
+    l.merges = (l.stream_parts * PAGE_STREAM_ROWS + l.tile_parts * PAGE_TILE_ROWS) / 8;
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;

@@ -28,7 +28,7 @@ void cut(int count, const int* cached, const int* rows, int hq, int hkv, int* ou
         if (w.tiles == 0) continue;
         const int kind = w.streamed ? 0 : 1, chunks = (w.blocks + range[kind] - 1) / range[kind];
         items[kind] += w.tiles * chunks;
-        if (chunks > 1) parts[kind] += w.tiles * chunks, merges += w.tiles;
+        if (chunks > 1) parts[kind] += w.tiles * chunks, merges += page_merge_entries(rows[r] * group, chunks);
         for (int t = 0; t < w.tiles; ++t) {  // the ranges of a tile cover what its rows see, once
             const int first = t * PAGE_TILE_ROWS, pairs = rows[r] * group;
             const int n = w.streamed ? pairs : (pairs - first < PAGE_TILE_ROWS ? pairs - first : PAGE_TILE_ROWS);

@@ -85,7 +85,7 @@ def test_short_steps_are_not_cut():
     cut, _ = _fits([(200, 1)] * 4, 32, 8, 128)
     assert cut["stream_parts"] == 0 and cut["merges"] == 0 and cut["stream_items"] == 4
     cut, _ = _fits([(131000, 1)], 32, 8, 128)
-    assert cut["stream_parts"] > 64 and cut["merges"] == 1
+    assert cut["stream_parts"] > 64 and cut["merges"] == 4
 
 
 # --------------------------------------------------------------------------- refusals: every call made here is refused, nothing is enqueued
