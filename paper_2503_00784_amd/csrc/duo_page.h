@@ -141,7 +141,8 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
     const bool ok = status == 0;
 
     // the cuts
-    const int range_s = page_range((long long)work[0], a.hkv, PAGE_STREAM_TARGET, PAGE_STREAM_MIN_BLOCKS);
+    const PageCut few = page_stream_cut(a.max_new, group);
+    const int range_s = page_range((long long)work[0], a.hkv, few.target, few.least);
     const int range_t = page_range((long long)work[1], a.hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS);
     enum { ITEM_S, ITEM_T, PART_S, PART_T, MERGE, CUTS };
     int cut[CUTS] = {};

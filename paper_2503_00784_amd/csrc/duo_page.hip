@@ -54,11 +54,12 @@ size_t layer_elems(const duo_model_config* cfg, const duo_page_cache* c) { retur
 
 template <int D>
 void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStream_t s) {
+    constexpr int TEAMS = D == 64 ? 2 : 1;
     const unsigned few = lay.stream_items * a.hkv;  // more workgroups than the plan has items end at once
     if (lay.tile_items > 0) DUO_LAUNCH((page_mixed_kernel<D>), dim3(lay.tile_items * a.hkv + few), dim3(256), s, a);
     else if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D>), dim3(few), dim3(256), s, a);
-    else if (lay.stream_rows <= 32) DUO_LAUNCH((page_team_kernel<D, 1>), dim3(few), dim3(128), s, a);
-    else DUO_LAUNCH((page_team_kernel<D, 2>), dim3(few), dim3(256), s, a);
+    else if (lay.stream_rows <= 32) DUO_LAUNCH((page_team_kernel<D, 1, TEAMS>), dim3(few), dim3(64 * TEAMS), s, a);
+    else DUO_LAUNCH((page_team_kernel<D, 2, TEAMS>), dim3(few), dim3(128 * TEAMS), s, a);
     if (lay.merges > 0) {
         const long long units = (long long)lay.merges * a.hkv;
         DUO_LAUNCH((page_merge_kernel<D>), dim3(units < 4096 ? (int)units : 4096), dim3(256), s, a);

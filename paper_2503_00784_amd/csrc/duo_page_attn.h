@@ -60,8 +60,11 @@ __device__ __forceinline__ PageItem page_item(const PageItem* p) {  // the same 
 }
 // 16 bytes per lane from global memory to LDS, lane after lane from `lds` on.  In assembly because of the waits: a wave that both requests
 // and reads LDS would otherwise wait for all of its requests in front of every read.  The wave waits for them itself (page_stage_landed).
+// ONCE: with the non-temporal hint, for what one workgroup alone reads.
+template <bool ONCE>
 __device__ __forceinline__ void page_load_lds(const u16* src, uint32_t lane_bytes, uint32_t lds) {  // src and lds the same in all lanes
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_bytes), "s"(src), "s"(lds) : "memory", "m0");
+    if (ONCE) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(lane_bytes), "s"(src), "s"(lds) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_bytes), "s"(src), "s"(lds) : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
@@ -72,6 +75,13 @@ template <int N>
 __device__ __forceinline__ void page_stage_landed() {
     static_assert(N >= 0 && N <= 63, "the memory counter has six bits");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The queries have come: waited for here, in front of a loop.  A wait for them inside it would be a wait for the newest request at every turn.
+template <int N>
+__device__ __forceinline__ void page_queries_landed(elem8 (&q)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(q[i]));
 }
 
 // Keeps a value's elements whose keys are below `valid` (of eight consecutive keys), the others become zero.
@@ -208,6 +218,7 @@ __global__ __launch_bounds__(256) void page_stream_kernel(PageAttnArgs a) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) qf[ks] = load_frag(qp + ks * 32);  // a column without a row takes the first row's and sees nothing
         }
+        page_queries_landed(qf);
         for (int i = 0; i < nb; ++i) {
             const int kb = (it.block0 + wave + NW * i) * 32;
             const bool masked = kb + 32 > sees_all;
@@ -515,19 +526,19 @@ struct PageBlocks {
 
 // ---- 17 to 64 rows: still the cache's bytes
 //
-// Two teams of UNITS waves, a wave for every 32 rows of the item.  Team z takes blocks z, z + 2, ...: a stage is a block for each team, put in LDS by
-// 16-byte loads from global memory to LDS one stage ahead of its use.  Two workgroups fit a compute unit, so that 64 KiB (heads of 128)
-// are in flight and one's start and end go under the other's loads.  The teams' states are joined through LDS.
-template <int D, int UNITS>
+// TEAMS teams of UNITS waves, a wave for every 32 rows of the item.  Team z takes blocks z, z + TEAMS, ...: a stage is a block for each team, put in
+// LDS by 16-byte loads from global memory to LDS one stage ahead of its use.  Several workgroups fit a compute unit, so that 64 KiB are in
+// flight and one's start and end go under the other's loads.  The teams' states are joined through LDS.  One team at heads of 128 (32 KiB of LDS
+// a workgroup): 16 x 33 rows of 32 heads 88 us with two, 81 with one; two at heads of 64.
+template <int D, int UNITS, int TEAMS>
 struct PageTeamLds {
-    static constexpr int TEAMS = 2, TILES = 2 * PageRows<D>::KT;
-    u32x4 kv[2][TEAMS * TILES * 64];
+    u32x4 kv[2][TEAMS * 2 * PageRows<D>::KT * 64];
     float ml[TEAMS][UNITS][2][32];
 };
-template <int D, int UNITS>
-__device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, int place, PageTeamLds<D, UNITS>& lds) {
+template <int D, int UNITS, int TEAMS>
+__device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, int place, PageTeamLds<D, UNITS, TEAMS>& lds) {
     using Rows = PageRows<D>;
-    constexpr int KT = Rows::KT, DT = Rows::DT, C32 = Rows::C32, TEAMS = PageTeamLds<D, UNITS>::TEAMS, TILES = KT + DT, PER_WAVE = TILES / UNITS;
+    constexpr int KT = Rows::KT, DT = Rows::DT, C32 = Rows::C32, TILES = KT + DT, PER_WAVE = TILES / UNITS;
     static_assert(TILES % UNITS == 0, "a team's waves move equal parts of its block");
     static_assert(sizeof(lds.kv) >= sizeof(f32x4) * TEAMS * UNITS * C32 * 4 * 64, "the teams' outputs fit");
     auto& lds_kv = lds.kv;
@@ -555,7 +566,7 @@ __device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, i
         for (int i = 0; i < PER_WAVE; ++i) {
             const int j = unit * PER_WAVE + i;
             const u16* src = j < KT ? a.kc + at + j * 512 : a.vc + at + (j - KT) * 512;
-            page_load_lds(src, lane * 16, lds_mine + (st & 1) * (TEAMS * TILES * 1024) + i * 1024);
+            page_load_lds<true>(src, lane * 16, lds_mine + (st & 1) * (TEAMS * TILES * 1024) + i * 1024);
         }
     };
     if (nst > 0) request(0);
@@ -563,6 +574,7 @@ __device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, i
     rows.load(a, it, hk, unit * 32, lane);
     const int sees_all = it.cached + (it.trunk > 0 ? 1 : 0);  // slots below are seen by every row
     bool odd = false;
+    page_queries_landed(rows.qf);
     for (int st = 0; st < nst; ++st) {
         page_stage_landed<0>();  // stage st is there, stage st - 1 drained
         if (st + 1 < nst) request(st + 1);
@@ -626,10 +638,10 @@ __device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, i
     }
     if (it.part >= 0 && team == 0 && half == 0) part[D] = top, part[D + 1] = sum;
 }
-template <int D, int UNITS>
-__global__ __launch_bounds__(128 * UNITS, 2) void page_team_kernel(PageAttnArgs a) {
-    __shared__ PageTeamLds<D, UNITS> lds;
-    page_team<D, UNITS>(a, a.stream, blockIdx.x, lds);
+template <int D, int UNITS, int TEAMS>
+__global__ __launch_bounds__(64 * TEAMS * UNITS, 2) void page_team_kernel(PageAttnArgs a) {
+    __shared__ PageTeamLds<D, UNITS, TEAMS> lds;
+    page_team<D, UNITS, TEAMS>(a, a.stream, blockIdx.x, lds);
 }
 
 // ---- many rows: the matrix units bound the time
@@ -672,15 +684,15 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
         const u16* k = a.kc + where.place<D>(__builtin_amdgcn_readlane(ids_k, st & 63), st * BPS + my_block + 1) + my_tile * 512;
         const u16* v = a.vc + where.place<D>(__builtin_amdgcn_readlane(ids_v, st & 63), st * BPS + my_block) + my_tile * 512;
 #pragma unroll
-        for (int i = 0; i < VPW; ++i) page_load_lds(v + i * 512, lane * 16, lds_v_mine + (st & 1) * (BPS * DT * 1024) + i * 1024);
+        for (int i = 0; i < VPW; ++i) page_load_lds<false>(v + i * 512, lane * 16, lds_v_mine + (st & 1) * (BPS * DT * 1024) + i * 1024);
 #pragma unroll
-        for (int i = 0; i < KPW; ++i) page_load_lds(k + i * 512, lane * 16, lds_k_mine + (st & 1) * (BPS * KT * 1024) + i * 1024);
+        for (int i = 0; i < KPW; ++i) page_load_lds<false>(k + i * 512, lane * 16, lds_k_mine + (st & 1) * (BPS * KT * 1024) + i * 1024);
     };
     if (nst > 0) {
         const int mine = wave * (KT / NW);  // block 0's keys are shared out among all four waves
         const u16* k = a.kc + where.place<D>(__builtin_amdgcn_readfirstlane(where.id(0)), 0) + mine * 512;
 #pragma unroll
-        for (int i = 0; i < KT / NW; ++i) page_load_lds(k + i * 512, lane * 16, lds_address(lds_k) + ((2 * BPS - 1) * KT + mine + i) * 1024);
+        for (int i = 0; i < KT / NW; ++i) page_load_lds<false>(k + i * 512, lane * 16, lds_address(lds_k) + ((2 * BPS - 1) * KT + mine + i) * 1024);
         request(0);
     }
     Rows rows;
@@ -773,12 +785,12 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void page_mixed_kernel(PageAttnArgs a) {
     __shared__ union Lds {
         PageTileLds<D> tile;
-        PageTeamLds<D, 2> team;
+        PageTeamLds<D, 2, 2> team;
         __device__ Lds() {}
     } lds;
     const int place = (int)blockIdx.x - a.tile_items * a.hkv;
     if (place < 0) page_tile<D>(a, a.tile, blockIdx.x, lds.tile);
-    else page_team<D, 2>(a, a.stream, place, lds.team);
+    else page_team<D, 2, 2>(a, a.stream, place, lds.team);
 }
 
 // ---- tiles whose keys were cut: the ranges' partial results of a row are joined in their order

@@ -11,8 +11,16 @@
 //   Tiled: more rows, tiles of PAGE_TILE_ROWS.  The matrix units bound the time, so the waves take different rows and share the blocks in LDS.
 constexpr int PAGE_STREAM_ROWS = 64;
 constexpr int PAGE_TILE_ROWS = 128;
-// Workgroups that the key ranges are cut for (fewer rows and requests than that are split over the keys), and the shortest ranges.
-constexpr int PAGE_STREAM_TARGET = 1024, PAGE_STREAM_MIN_BLOCKS = 8;
+// Workgroups that the key ranges are cut for (fewer rows and requests than that are split over the keys), and the shortest ranges.  Streamed requests
+// of more than 16 rows at most: 512 and 16, since their partial results are what a range costs (16 x 33 rows of 32 heads: 81 us, 94 with
+// 1024; 9 rows * 4 behind 30000 keys: 34, 45 with ranges of 32 blocks); of fewer: 1024 and 8 (8 requests behind 1500 keys: 14.4 us, 18.7 with
+// ranges of 32).
+struct PageCut {
+    int target, least;
+};
+__host__ __device__ __forceinline__ PageCut page_stream_cut(int max_new, int group) {
+    return (long long)max_new * group <= 16 ? PageCut{1024, 8} : PageCut{512, 16};
+}
 constexpr int PAGE_TILE_TARGET = 512, PAGE_TILE_MIN_BLOCKS = 16;
 
 // Limits that keep every sum of a plan inside 32 bits: 4096 requests of 2^18 rows, 2^18 pages or 2^18 blocks each.
@@ -59,8 +67,9 @@ inline PageLayout page_layout(int requests, int max_rows, int max_new, int max_b
     const int group = hq / hkv;
     const bool tiles_possible = (long long)max_new * group > PAGE_STREAM_ROWS;
     PageLayout l;
-    l.stream_items = PAGE_STREAM_TARGET / hkv + requests;
-    l.stream_parts = max_blocks > PAGE_STREAM_MIN_BLOCKS ? 2 * PAGE_STREAM_TARGET / hkv : 0;
+    const PageCut cut = page_stream_cut(max_new, group);
+    l.stream_items = cut.target / hkv + requests;
+    l.stream_parts = max_blocks > cut.least ? 2 * cut.target / hkv : 0;
     // a tiled request has more than PAGE_STREAM_ROWS rows
     const long long all = (long long)max_rows * group;
     const long long tiled_requests = all / (PAGE_STREAM_ROWS + 1) < requests ? all / (PAGE_STREAM_ROWS + 1) : requests;
