@@ -474,12 +474,28 @@ class VerifyEngine:
         return out
 
 
+def _held_in(*names):
+    """Properties that read self._<name>: what the C structs made once point to cannot be exchanged behind their back."""
+    def decorate(cls):
+        for name in names:
+            setattr(cls, name, property(lambda self, _n="_" + name: getattr(self, _n)))
+        return cls
+    return decorate
+
+
+@_held_in("block_table", "held", "free_pages", "free_count")
 class PageTables:
     """Who holds which page (duo_page_tables): int32 device tensors block_table [requests][max_pages], held [requests],
-    free_pages [n_pages], free_count [1]."""
+    free_pages [n_pages], free_count [1].  The tensors' contents change, the tensors do not."""
 
     def __init__(self, block_table, held, free_pages, free_count):
-        self.block_table, self.held, self.free_pages, self.free_count = block_table, held, free_pages, free_count
+        import torch
+        self._block_table, self._held, self._free_pages, self._free_count = block_table, held, free_pages, free_count
+        for name, t in zip(("block_table", "held", "free_pages", "free_count"), self.tensors()):
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != block_table.device:
+                raise ValueError(f"{name} must be contiguous int32 on {block_table.device}, not {t.dtype} on {t.device}")
+        self.dims = tuple(tuple(t.shape) for t in self.tensors())
+        self.c = PageTablesC(*[t.data_ptr() for t in self.tensors()])
 
     @classmethod
     def empty(cls, requests: int, max_pages: int, n_pages: int, device) -> "PageTables":
@@ -490,12 +506,10 @@ class PageTables:
                    torch.full((1,), n_pages, **i32))
 
     def tensors(self):
-        return self.block_table, self.held, self.free_pages, self.free_count
-
-    def c(self) -> PageTablesC:
-        return PageTablesC(*[t.data_ptr() for t in self.tensors()])
+        return self._block_table, self._held, self._free_pages, self._free_count
 
 
+@_held_in("key_pages", "value_pages", "cached", "trunk", "n", "k", "row_start", "position", "slot", "status", "workspace")
 class PagedCache:
     """Keys and values of many requests in pages of a common pool, and the calls of a step over them (the duo_page_* entry
     points of include/duo_verify.h): plan, then append and attention for every layer, then commit.
@@ -511,25 +525,33 @@ class PagedCache:
         self.torch = torch
         self.shape, self.dtype = shape, dtype
         self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device(self.device.type, torch.cuda.current_device() if self.device.type == "cuda" else 0)
+        if self.device.index is None and self.device.type == "cuda":
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.lib = load(dtype)
         self.cfg = make_config(shape, 32)
         self.max_requests, self.max_rows = int(max_requests), int(max_rows)
         self.max_new = self.max_rows if max_new is None else int(max_new)
         self.n_pages, self.page_slots, self.max_pages = int(n_pages), int(page_slots), int(max_pages)
         self.ws_bytes = self._workspace_bytes()  # refuses what the library does not take, before anything is allocated
-        i32 = dict(dtype=torch.int32, device=device)
+        i32 = dict(dtype=torch.int32, device=self.device)
         dims = (shape.n_layers, self.n_pages, shape.n_kv_heads, self.page_slots * shape.head_dim)
-        self.key_pages = torch.zeros(dims, dtype=torch.int16, device=device)
-        self.value_pages = torch.zeros(dims, dtype=torch.int16, device=device)
-        self.tables = PageTables.empty(self.max_requests, self.max_pages, self.n_pages, device)
-        self.cached, self.trunk, self.n, self.k = (torch.zeros(self.max_requests, **i32) for _ in range(4))
-        self.row_start = torch.zeros(self.max_requests + 1, **i32)
-        self.position, self.slot = (torch.full((self.max_rows,), -1, **i32) for _ in range(2))
-        self.status = torch.zeros(1, **i32)
-        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
+        self._key_pages = torch.zeros(dims, dtype=torch.int16, device=self.device)
+        self._value_pages = torch.zeros(dims, dtype=torch.int16, device=self.device)
+        self._cached, self._trunk, self._n, self._k = (torch.zeros(self.max_requests, **i32) for _ in range(4))
+        self._row_start = torch.zeros(self.max_requests + 1, **i32)
+        self._position, self._slot = (torch.full((self.max_rows,), -1, **i32) for _ in range(2))
+        self._status = torch.zeros(1, **i32)
+        self._workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
         self._planned = self.max_requests
+        self._element_types = (torch.float16 if dtype == "fp16" else torch.bfloat16, torch.int16)
+        # the C structs of every call, made once
+        self._cache_c = PageCacheC(self._key_pages.data_ptr(), self._value_pages.data_ptr(), self.n_pages, self.page_slots, self.max_pages)
+        self._batch_c = PageBatchC(*[t.data_ptr() for t in (self._cached, self._trunk, self._n, self._k, self._row_start, self._position, self._slot, self._status)],
+                                   self.max_requests, self.max_rows, self.max_new)
+        self._refs = C.byref(self.cfg), C.byref(self._cache_c), C.byref(self._batch_c)
+        self._ws_ptr = self._workspace.data_ptr()
+        self._head_dim, self._hq, self._hkv = shape.head_dim, shape.n_q_heads, shape.n_kv_heads
+        self.tables = PageTables.empty(self.max_requests, self.max_pages, self.n_pages, self.device)
 
     def _workspace_bytes(self) -> int:
         out = C.c_size_t(0)
@@ -538,102 +560,93 @@ class PagedCache:
         _check(self.lib.duo_page_workspace_bytes(C.byref(self.cfg), C.byref(cache), C.byref(batch), C.byref(out)), "duo_page_workspace_bytes")
         return out.value
 
-    def _cache_c(self) -> PageCacheC:
-        return PageCacheC(self.key_pages.data_ptr(), self.value_pages.data_ptr(), self.n_pages, self.page_slots, self.max_pages)
+    def _fits(self, t: PageTables) -> PageTables:
+        want = ((self.max_requests, self.max_pages), (self.max_requests,), (self.n_pages,), (1,))
+        if t.dims != want or t.block_table.device != self.device:
+            raise ValueError(f"tables of {t.dims} on {t.block_table.device}, the cache's are {want} on {self.device}")
+        return t
 
-    def _batch_c(self, n_requests: int) -> PageBatchC:
-        return PageBatchC(*[t.data_ptr() for t in (self.cached, self.trunk, self.n, self.k, self.row_start, self.position, self.slot, self.status)],
-                          n_requests, self.max_rows, self.max_new)
+    @property
+    def tables(self) -> PageTables:
+        return self._tables
 
-    def _stream(self):
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+    @tables.setter
+    def tables(self, t: PageTables) -> None:
+        self._tables = self._fits(t)
+        self._tables_ref, self._table_ptr = C.byref(t.c), t.block_table.data_ptr()
+
+    def _call(self, name: str, *args) -> None:
+        """The entry point with the cache's device current, on that device's current stream."""
+        torch, function = self.torch, getattr(self.lib, name)
+        index = self.device.index
+        if index == torch.cuda.current_device():
+            rc = function(*args, torch.cuda.current_stream().cuda_stream)
+        else:
+            with torch.cuda.device(index):
+                rc = function(*args, torch.cuda.current_stream().cuda_stream)
+        if rc:
+            _check(rc, name)
 
     def _rows(self, name: str, t, heads: int, writes: bool = False):
         """A matrix of the step's rows, [max_rows][heads * head_dim] or [max_rows][heads][head_dim], rows any distance apart: (pointer, distance)."""
-        D = self.shape.head_dim
-        want = self.torch.float16 if self.dtype == "fp16" else self.torch.bfloat16
-        if t.dtype not in (want, self.torch.int16) or t.device != self.device:
-            raise ValueError(f"{name} must be {want} or int16 bit patterns on {self.device}, not {t.dtype} on {t.device}")
-        if tuple(t.shape) not in ((self.max_rows, heads * D), (self.max_rows, heads, D)):
-            raise ValueError(f"{name} must be [{self.max_rows}][{heads} * {D}], not {list(t.shape)}")
-        if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != D):
+        D, shape, stride = self._head_dim, t.shape, t.stride()
+        if t.dtype not in self._element_types or t.device != self.device:
+            raise ValueError(f"{name} must be {self._element_types[0]} or int16 bit patterns on {self.device}, not {t.dtype} on {t.device}")
+        if shape != (self.max_rows, heads * D) and shape != (self.max_rows, heads, D):
+            raise ValueError(f"{name} must be [{self.max_rows}][{heads} * {D}], not {list(shape)}")
+        if stride[-1] != 1 or (len(stride) == 3 and heads > 1 and stride[1] != D):
             raise ValueError(f"{name}: the elements of a row must lie together")
-        stride = t.stride(0) if self.max_rows > 1 else heads * D
-        if writes and stride < heads * D:
+        distance = stride[0] if self.max_rows > 1 else heads * D
+        if writes and distance < heads * D:
             raise ValueError(f"{name}: rows overlap")
-        return t.data_ptr(), stride
-
-    def _ints(self, name: str, t, dims):
-        if t.dtype != self.torch.int32 or t.device != self.device or tuple(t.shape) != tuple(dims) or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous int32 {list(dims)} on {self.device}, not {t.dtype} {list(t.shape)} on {t.device}")
-        return t.data_ptr()
+        return t.data_ptr(), distance
 
     def set_requests(self, trunk: Sequence[int], n: Sequence[int], k: Sequence[int], cached: Optional[Sequence[int]] = None) -> None:
         """What the requests bring to the next step, from the host; `cached` only where it is not what the commits left."""
-        for dst, src in ((self.trunk, trunk), (self.n, n), (self.k, k), (self.cached, cached)):
+        for dst, src in ((self._trunk, trunk), (self._n, n), (self._k, k), (self._cached, cached)):
             if src is not None:
                 src = self.torch.tensor(list(src), dtype=self.torch.int32)
                 if len(src) > self.max_requests:
                     raise ValueError(f"{len(src)} requests, the cache has room for {self.max_requests}")
                 dst[:len(src)] = src.to(self.device)
 
-    def _count(self, n_requests: Optional[int]) -> int:
+    def plan(self, n_requests: Optional[int] = None, source: Optional[PageTables] = None) -> None:
+        """Enqueue the plan of a step of the first n_requests requests (default: all there is room for).  `source`: the tables to
+        start from, left as they are (`tables` receives the result); default `tables`, in place."""
         n = self.max_requests if n_requests is None else int(n_requests)
         if not 1 <= n <= self.max_requests:
             raise ValueError(f"{n} requests, the cache has room for {self.max_requests}")
-        return n
-
-    def plan(self, n_requests: Optional[int] = None, source: Optional[PageTables] = None) -> None:
-        """Enqueue the plan of a step of the first n_requests requests.  `source`: the tables to start from, left as they are
-        (`tables` receives the result); default `tables`, in place."""
-        n = self._count(n_requests)
-        src = self.tables if source is None else source
-        for t in (src, self.tables):
-            self._ints("block_table", t.block_table, (self.max_requests, self.max_pages))
-            self._ints("held", t.held, (self.max_requests,))
-            self._ints("free_pages", t.free_pages, (self.n_pages,))
-            self._ints("free_count", t.free_count, (1,))
-        with self.torch.cuda.device(self.device):
-            rc = self.lib.duo_page_plan(C.byref(self.cfg), C.byref(self._cache_c()), C.byref(src.c()), C.byref(self.tables.c()), C.byref(self._batch_c(n)),
-                                        self.workspace.data_ptr(), self.ws_bytes, self._stream())
-        _check(rc, "duo_page_plan")
-        self._planned = n
+        src = self._tables_ref if source is None else C.byref(self._fits(source).c)
+        cfg, cache, batch = self._refs
+        self._batch_c.n_requests = self._planned = n
+        self._call("duo_page_plan", cfg, cache, src, self._tables_ref, batch, self._ws_ptr, self.ws_bytes)
 
     def append(self, layer: int, q, k, v, q_out=None):
         """Enqueue the rotary embedding of q and k and the writing of k and v into the pages; returns q_out (default: in place)."""
         q_out = q if q_out is None else q_out
-        hq, hkv = self.shape.n_q_heads, self.shape.n_kv_heads
-        args = [x for t in (self._rows("q", q, hq), self._rows("k", k, hkv), self._rows("v", v, hkv), self._rows("q_out", q_out, hq, True)) for x in t]
-        with self.torch.cuda.device(self.device):
-            rc = self.lib.duo_page_append(C.byref(self.cfg), C.byref(self._cache_c()), C.byref(self._batch_c(self._planned)), int(layer), *args, self._stream())
-        _check(rc, "duo_page_append")
+        hkv = self._hkv
+        qa, ka, va, oa = self._rows("q", q, self._hq), self._rows("k", k, hkv), self._rows("v", v, hkv), self._rows("q_out", q_out, self._hq, True)
+        self._call("duo_page_append", *self._refs, int(layer), *qa, *ka, *va, *oa)
         return q_out
 
     def attention(self, layer: int, q, out=None, scale: float = 0.0):
         """Enqueue the attention of the planned rows (rotated queries, as `append` leaves them); returns out."""
-        hq = self.shape.n_q_heads
         if out is None:
             out = self.torch.zeros_like(q, memory_format=self.torch.contiguous_format)
-        args = [x for t in (self._rows("q", q, hq), self._rows("out", out, hq, True)) for x in t]
-        with self.torch.cuda.device(self.device):
-            rc = self.lib.duo_page_attention(C.byref(self.cfg), C.byref(self._cache_c()), self.tables.block_table.data_ptr(),
-                                             C.byref(self._batch_c(self._planned)), int(layer), *args, float(scale), self.workspace.data_ptr(),
-                                             self.ws_bytes, self._stream())
-        _check(rc, "duo_page_attention")
+        cfg, cache, batch = self._refs
+        self._call("duo_page_attention", cfg, cache, self._table_ptr, batch, int(layer), *self._rows("q", q, self._hq),
+                   *self._rows("out", out, self._hq, True), scale, self._ws_ptr, self.ws_bytes)
         return out
 
     def commit(self, records, cached_out=None) -> None:
         """Enqueue the commit: records int32 [requests][4] as the samplers write them; the new lengths go to `cached`, or to cached_out."""
-        out = self.cached if cached_out is None else cached_out
-        self._ints("records", records, (self._planned, 4))
-        self._ints("cached_out", out, (out.shape[0],))
-        if out.shape[0] < self._planned:
-            raise ValueError(f"cached_out has room for {out.shape[0]} of {self._planned} requests")
-        with self.torch.cuda.device(self.device):
-            rc = self.lib.duo_page_commit(C.byref(self.cfg), C.byref(self._cache_c()), self.tables.block_table.data_ptr(),
-                                          C.byref(self._batch_c(self._planned)), records.data_ptr(), out.data_ptr(), self.workspace.data_ptr(),
-                                          self.ws_bytes, self._stream())
-        _check(rc, "duo_page_commit")
+        out, i32 = self._cached if cached_out is None else cached_out, self.torch.int32
+        if records.dtype != i32 or records.device != self.device or records.shape != (self._planned, 4) or not records.is_contiguous():
+            raise ValueError(f"records must be contiguous int32 [{self._planned}][4] on {self.device}, not {records.dtype} {list(records.shape)} on {records.device}")
+        if out.dtype != i32 or out.device != self.device or out.dim() != 1 or out.shape[0] < self._planned or not out.is_contiguous():
+            raise ValueError(f"cached_out must be contiguous int32 [{self._planned}] on {self.device}, not {out.dtype} {list(out.shape)} on {out.device}")
+        cfg, cache, batch = self._refs
+        self._call("duo_page_commit", cfg, cache, self._table_ptr, batch, records.data_ptr(), out.data_ptr(), self._ws_ptr, self.ws_bytes)
 
 
 def spec_sample(logits, root_logits, draft_tokens, draft_probs, uniforms, temperature: float = 1.0,

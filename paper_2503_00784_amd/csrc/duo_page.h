@@ -303,73 +303,119 @@ struct PageAppendArgs {
     const int32_t *position, *slot;
     int32_t* status;
     int32_t rows, hq, hkv, page_shift, n_pages;
+    int32_t heads_each, rope_groups;
     double turns[64];  // theta^(-2d/D) / 2 pi: turns per position
 };
 
-// A thread takes eight channels and their eight rotary partners of one (row, head): two 16-byte loads and stores; K's eight channels of a
-// slot are one 16-byte piece of a tile.  The angle is reduced in double precision (position times turns keeps 2^-53 of up to
-// 2^23 positions), the sine and cosine of the remainder are fp32.
-template <int D>
-__global__ __launch_bounds__(256) void page_rope_kernel(PageAppendArgs a) {
-    constexpr int TPH = D / 16;  // threads per head
-    const int heads = a.hq + a.hkv;
-    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    const int part = (int)(i % TPH);
-    const long long j = i / TPH;
-    const int head = (int)(j % heads);
-    const long long row = j / heads;
-    if (row >= a.rows) return;
-    const int slot = a.slot[row];
-    if (slot < 0) return;
-    const int page = slot >> a.page_shift;
-    const bool bad = page >= a.n_pages;
-    const double pos = (double)a.position[row];
-    const u16* src = head < a.hq ? a.q + row * a.q_stride + head * D : a.k + row * a.k_stride + (head - a.hq) * D;
-    src += part * 8;
-    Frag8 x, y, xo, yo;
-    x.q = *reinterpret_cast<const u32x4*>(src);
-    y.q = *reinterpret_cast<const u32x4*>(src + D / 2);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const double t = pos * a.turns[part * 8 + e];
-        float s, c;
-        sincospif(2.0f * (float)(t - floor(t)), &s, &c);
-        const float xf = elem_to_f32(x.h[e]), yf = elem_to_f32(y.h[e]);
-        xo.h[e] = f32_to_elem(xf * c - yf * s);
-        yo.h[e] = f32_to_elem(yf * c + xf * s);
-    }
-    if (head < a.hq) {
-        u16* dst = a.q_out + row * a.q_out_stride + head * D + part * 8;
-        *reinterpret_cast<u32x4*>(dst) = xo.q;
-        *reinterpret_cast<u32x4*>(dst + D / 2) = yo.q;
-    } else if (!bad) {
-        const int in_page = slot & ((1 << a.page_shift) - 1);
-        u16* plane = a.kc + (((size_t)page * a.hkv + (head - a.hq)) << a.page_shift) * D;
-        *reinterpret_cast<u32x4*>(plane + k_cache_offset(D, in_page, part * 8)) = xo.q;
-        *reinterpret_cast<u32x4*>(plane + k_cache_offset(D, in_page, part * 8 + D / 2)) = yo.q;
-    } else if (part == 0) {
-        atomicOr(a.status, DUO_PAGE_BAD_PAGE);
-    }
-}
+// A workgroup takes 32 rows: blockIdx.y < rope_groups: `heads_each` query and key heads, otherwise one head's values.  What bounds it at many rows is
+// the bytes.
+//
+// Rotation: a thread takes eight channels and their eight partners of a row, forms their angles once and goes through the heads: two 16-byte
+// loads and stores each; K's eight channels of a slot are one 16-byte piece of a tile.  The angle is reduced in double precision (position
+// times turns keeps 2^-53 of up to 2^23 positions), sine and cosine of the remainder are fp32.
+//
+// Values: a tile holds eight consecutive slots of a channel together.  Eight rows in a row that fill such a piece (all but the ends of a
+// request's rows) are turned around through LDS and written 16 bytes a channel; other rows two bytes a channel.  A workgroup sees to the pieces
+// that start in its rows, so it reads up to seven rows more.
+//
+// 8410 rows of 32 query and 8 key heads of 128: 35 us (5.8 TB/s of what is read and written once; a copy reaches 4.9); 80 with a sine and cosine for
+// every head and two bytes a channel throughout.
+constexpr int PAGE_APPEND_ROWS = 32;
 
 template <int D>
-__global__ __launch_bounds__(256) void page_values_kernel(PageAppendArgs a) {
-    constexpr int TPH = D / 8;
-    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    const int part = (int)(i % TPH);
-    const long long j = i / TPH;
-    const int head = (int)(j % a.hkv);
-    const long long row = j / a.hkv;
+__device__ __forceinline__ void page_rope(const PageAppendArgs& a) {
+    constexpr int TPH = D / 16, HPP = 256 / (PAGE_APPEND_ROWS * TPH);  // threads per row and head, heads at a time
+    const int part = threadIdx.x % TPH, row = blockIdx.x * PAGE_APPEND_ROWS + threadIdx.x / TPH % PAGE_APPEND_ROWS;
     if (row >= a.rows) return;
     const int slot = a.slot[row];
     if (slot < 0) return;
     const int page = slot >> a.page_shift, in_page = slot & ((1 << a.page_shift) - 1);
-    if (page >= a.n_pages) return;
-    Frag8 x;
-    x.q = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + head * D + part * 8);
-    u16* plane = a.vc + (((size_t)page * a.hkv + head) << a.page_shift) * D;
+    const bool known = page < a.n_pages;
+    const double pos = (double)a.position[row];
+    float sn[8], cs[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) plane[v_cache_offset(D, in_page, part * 8 + e)] = x.h[e];
+    for (int e = 0; e < 8; ++e) {
+        const double t = pos * a.turns[part * 8 + e];
+        sincospif(2.0f * (float)(t - floor(t)), &sn[e], &cs[e]);
+    }
+    const int last = min((int)(blockIdx.y + 1) * a.heads_each, a.hq + a.hkv);
+    for (int head = blockIdx.y * a.heads_each + threadIdx.x / (TPH * PAGE_APPEND_ROWS); head < last; head += HPP) {
+        const u16* src = head < a.hq ? a.q + (size_t)row * a.q_stride + head * D : a.k + (size_t)row * a.k_stride + (head - a.hq) * D;
+        src += part * 8;
+        Frag8 x, y, xo, yo;
+        x.q = *reinterpret_cast<const u32x4*>(src);
+        y.q = *reinterpret_cast<const u32x4*>(src + D / 2);
+        float xf[8], yf[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float u = elem_to_f32(x.h[e]), v = elem_to_f32(y.h[e]);
+            xf[e] = u * cs[e] - v * sn[e];
+            yf[e] = v * cs[e] + u * sn[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) xo.q[e] = pack_elem2(xf[2 * e], xf[2 * e + 1]), yo.q[e] = pack_elem2(yf[2 * e], yf[2 * e + 1]);
+        if (head < a.hq) {
+            u16* dst = a.q_out + (size_t)row * a.q_out_stride + head * D + part * 8;
+            *reinterpret_cast<u32x4*>(dst) = xo.q;
+            *reinterpret_cast<u32x4*>(dst + D / 2) = yo.q;
+        } else if (known) {
+            u16* plane = a.kc + (((size_t)page * a.hkv + (head - a.hq)) << a.page_shift) * D;
+            *reinterpret_cast<u32x4*>(plane + k_cache_offset(D, in_page, part * 8)) = xo.q;
+            *reinterpret_cast<u32x4*>(plane + k_cache_offset(D, in_page, part * 8 + D / 2)) = yo.q;
+        } else if (part == 0) {
+            atomicOr(a.status, DUO_PAGE_BAD_PAGE);
+        }
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void page_values(const PageAppendArgs& a) {
+    constexpr int R = PAGE_APPEND_ROWS, SEEN = R + 7, CHUNKS = D / 8, PAD = D + 2;
+    __shared__ u16 v[SEEN * PAD];
+    __shared__ int slots[7 + SEEN], pieces[R], singles[R], counts[2];
+    const int head = blockIdx.y - a.rope_groups, row0 = blockIdx.x * R;
+    if (threadIdx.x < 2) counts[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < 7 + SEEN; i += blockDim.x) {  // rows row0 - 7 .. row0 + R + 6
+        const int row = row0 - 7 + i;
+        int s = row >= 0 && row < a.rows ? a.slot[row] : -1;
+        slots[i] = s >= 0 && s >> a.page_shift < a.n_pages ? s : -1;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < SEEN * CHUNKS; i += blockDim.x) {
+        const int r = i / CHUNKS, d = i % CHUNKS * 8;
+        if (slots[7 + r] < 0) continue;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a.v + (size_t)(row0 + r) * a.v_stride + head * D + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&v[r * PAD + d + 2 * e]) = x[e];
+    }
+    if (threadIdx.x < R && slots[7 + threadIdx.x] >= 0) {
+        const int s = slots[7 + threadIdx.x], first = 7 + threadIdx.x - (s & 7);  // where the row's piece would start
+        bool whole = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) whole &= slots[first + e] == (s & ~7) + e;
+        if (!whole) singles[atomicAdd(&counts[1], 1)] = threadIdx.x;  // the order of the lists does not matter
+        else if ((s & 7) == 0) pieces[atomicAdd(&counts[0], 1)] = threadIdx.x;
+    }
+    __syncthreads();
+    auto plane = [&](int s) { return a.vc + (((size_t)(s >> a.page_shift) * a.hkv + head) << a.page_shift) * D; };
+    const int mask = (1 << a.page_shift) - 1;
+    for (int i = threadIdx.x; i < counts[0] * D; i += blockDim.x) {
+        const int r = pieces[i / D], d = i % D, s = slots[7 + r];
+        Frag8 f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.h[e] = v[(r + e) * PAD + d];
+        *reinterpret_cast<u32x4*>(plane(s) + v_cache_offset(D, s & mask, d)) = f.q;
+    }
+    for (int i = threadIdx.x; i < counts[1] * D; i += blockDim.x) {
+        const int r = singles[i / D], d = i % D, s = slots[7 + r];
+        plane(s)[v_cache_offset(D, s & mask, d)] = v[r * PAD + d];
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void page_append_kernel(PageAppendArgs a) {
+    if ((int)blockIdx.y < a.rope_groups) page_rope<D>(a);
+    else page_values<D>(a);
 }
 
 // ---- commit
@@ -387,12 +433,16 @@ __device__ __forceinline__ bool page_plan_is(const PageHeader& h, int requests, 
            h.max_pages == max_pages && h.max_rows == max_rows && h.max_new == max_new;
 }
 
-// One workgroup per (request, layer, kv head).  K: a slot's eight channels are a 16-byte piece; V: a channel's slots are two bytes each.  Source and
-// target share no slot (branch 0 lies where it belongs, branch i >= 1 starts i * k >= a slots further on).
+// One workgroup per (request, layer, kv head).  K: a slot's eight channels are a 16-byte piece; V: eight slots of a channel are, read as such and
+// written two bytes each, since source and target lie differently in theirs.  Source and target share no slot (branch 0 lies where it belongs,
+// branch i >= 1 starts i * k >= a slots further on).  What bounds it is three dependent round trips: plan and record, page ids, data.
+// 48 requests, 16 layers of 8 heads: 18 us with a load and two page lookups for every value, 15 so.
 template <int D>
 __global__ __launch_bounds__(128) void page_commit_kernel(PageCommitArgs a) {
-    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
     const int r = blockIdx.x, layer = blockIdx.y, head = blockIdx.z;
+    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    const PageInfo p = reinterpret_cast<const PageInfo*>(a.ws + a.info)[r];  // of no meaning without a plan
+    const int branch = a.records[4 * r], accepted = a.records[4 * r + 1], token = a.records[4 * r + 2];
     const bool first = layer == 0 && head == 0 && threadIdx.x == 0;
     const bool known = page_plan_is(hdr, a.requests, a.hq, a.hkv, D, a.page_shift, a.max_pages, a.max_rows, a.max_new);
     if (!known || !hdr.ok) {
@@ -402,21 +452,16 @@ __global__ __launch_bounds__(128) void page_commit_kernel(PageCommitArgs a) {
         }
         return;
     }
-    const PageInfo p = reinterpret_cast<const PageInfo*>(a.ws + a.info)[r];
-    const int branch = a.records[4 * r], accepted = a.records[4 * r + 1], token = a.records[4 * r + 2];
-    const int branches = p.k > 0 ? p.n : 0;
     int moved = 0, after = p.cached + p.trunk;
-    if (branches > 0) {
-        const bool none = branch < 0;
-        if (none ? token < 0 : false) after = p.cached;
-        else if (!none) {
-            if (branch >= branches || accepted < 0 || accepted > p.k) {
-                after = p.cached;
-                if (first) atomicOr(a.status, DUO_PAGE_BAD_RECORD);
-            } else {
-                after += accepted;
-                moved = branch > 0 ? accepted : 0;
-            }
+    if (p.n > 0 && p.k > 0) {
+        if (branch >= p.n || (branch >= 0 && (accepted < 0 || accepted > p.k))) {
+            after = p.cached;
+            if (first) atomicOr(a.status, DUO_PAGE_BAD_RECORD);
+        } else if (branch < 0) {
+            if (token < 0) after = p.cached;
+        } else {
+            after += accepted;
+            moved = branch > 0 ? accepted : 0;
         }
     }
     if (first) a.cached_out[r] = after;
@@ -424,28 +469,41 @@ __global__ __launch_bounds__(128) void page_commit_kernel(PageCommitArgs a) {
     const int to0 = p.cached + p.trunk, from0 = to0 + branch * p.k;
     const int32_t* line = a.table + (size_t)r * a.max_pages;
     const size_t layer_pages = (size_t)layer * a.n_pages;
-    auto plane = [&](u16* base, int logical, bool& fine) {
-        const int page = line[logical >> a.page_shift];
-        fine = (unsigned)page < (unsigned)a.n_pages;
-        return base + (((layer_pages + (fine ? page : 0)) * a.hkv + head) << a.page_shift) * D;
-    };
     const int mask = (1 << a.page_shift) - 1;
+    auto page_at = [&](int logical) {
+        const int page = line[logical >> a.page_shift];
+        const bool fine = (unsigned)page < (unsigned)a.n_pages;
+        if (!fine) atomicOr(a.status, DUO_PAGE_BAD_PAGE);
+        return fine ? page : -1;
+    };
+    auto plane = [&](u16* base, int page) { return base + (((layer_pages + page) * a.hkv + head) << a.page_shift) * D; };
+    // the targets lie in one page or two as a rule: looked up once, like the source's first and last
+    const int to_page0 = page_at(to0), to_page1 = page_at(to0 + moved - 1), from_page0 = page_at(from0), from_page1 = page_at(from0 + moved - 1);
+    auto page_of = [&](int logical, int first, int last, int page0, int page1) {
+        const int at = logical >> a.page_shift;
+        return at == first >> a.page_shift ? page0 : at == last >> a.page_shift ? page1 : page_at(logical);
+    };
+    auto to_page = [&](int logical) { return page_of(logical, to0, to0 + moved - 1, to_page0, to_page1); };
+    auto from_page = [&](int logical) { return page_of(logical, from0, from0 + moved - 1, from_page0, from_page1); };
     constexpr int KP = D / 8;
     for (int i = threadIdx.x; i < moved * KP; i += blockDim.x) {
-        const int j = i / KP, d = i % KP * 8;
-        bool ok0, ok1;
-        u16* const src = plane(a.kc, from0 + j, ok0);
-        u16* const dst = plane(a.kc, to0 + j, ok1);
-        if (ok0 && ok1)
-            *reinterpret_cast<u32x4*>(dst + k_cache_offset(D, (to0 + j) & mask, d)) =
-                *reinterpret_cast<const u32x4*>(src + k_cache_offset(D, (from0 + j) & mask, d));
-        else atomicOr(a.status, DUO_PAGE_BAD_PAGE);
+        const int j = i / KP, d = i % KP * 8, from = from_page(from0 + j), to = to_page(to0 + j);
+        if (from >= 0 && to >= 0)
+            *reinterpret_cast<u32x4*>(plane(a.kc, to) + k_cache_offset(D, (to0 + j) & mask, d)) =
+                *reinterpret_cast<const u32x4*>(plane(a.kc, from) + k_cache_offset(D, (from0 + j) & mask, d));
     }
-    for (int i = threadIdx.x; i < moved * D; i += blockDim.x) {
-        const int j = i / D, d = i % D;
-        bool ok0, ok1;
-        u16* const src = plane(a.vc, from0 + j, ok0);
-        u16* const dst = plane(a.vc, to0 + j, ok1);
-        if (ok0 && ok1) dst[v_cache_offset(D, (to0 + j) & mask, d)] = src[v_cache_offset(D, (from0 + j) & mask, d)];
+    const int group0 = from0 >> 3, groups = ((from0 + moved - 1) >> 3) - group0 + 1;
+    for (int i = threadIdx.x; i < groups * D; i += blockDim.x) {
+        const int d = i % D, slot0 = (group0 + i / D) * 8, from = from_page(slot0);  // a group lies in one page
+        if (from < 0) continue;
+        Frag8 f;
+        f.q = *reinterpret_cast<const u32x4*>(plane(a.vc, from) + v_cache_offset(D, slot0 & mask, d));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int j = slot0 + e - from0;
+            if (j < 0 || j >= moved) continue;
+            const int to = to_page(to0 + j);
+            if (to >= 0) plane(a.vc, to)[v_cache_offset(D, (to0 + j) & mask, d)] = f.h[e];
+        }
     }
 }

@@ -132,15 +132,14 @@ extern "C" int duo_page_append(const duo_model_config* cfg, const duo_page_cache
     for (int d = 0; d < D / 2; ++d) a.turns[d] = pow((double)cfg->rope_theta, -2.0 * d / D) / (2.0 * M_PI);
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // not of an earlier call
-    const long long rope = (long long)b->max_rows * (cfg->n_q_heads + cfg->n_kv_heads) * (D / 16), vals = (long long)b->max_rows * cfg->n_kv_heads * (D / 8);
-    const dim3 gr((unsigned)((rope + 255) / 256)), gv((unsigned)((vals + 255) / 256));
-    if (D == 64) {
-        DUO_LAUNCH((page_rope_kernel<64>), gr, dim3(256), s, a);
-        DUO_LAUNCH((page_values_kernel<64>), gv, dim3(256), s, a);
-    } else {
-        DUO_LAUNCH((page_rope_kernel<128>), gr, dim3(256), s, a);
-        DUO_LAUNCH((page_values_kernel<128>), gv, dim3(256), s, a);
-    }
+    // Heads that share a row's angles: as many as leave 1024 workgroups, at most eight.
+    const int windows = (b->max_rows + PAGE_APPEND_ROWS - 1) / PAGE_APPEND_ROWS, heads = cfg->n_q_heads + cfg->n_kv_heads;
+    const long long each = (long long)windows * heads / 1024;
+    a.heads_each = each < 1 ? 1 : each > 8 ? 8 : (int)each;
+    a.rope_groups = (heads + a.heads_each - 1) / a.heads_each;
+    const dim3 grid(windows, a.rope_groups + cfg->n_kv_heads);
+    if (D == 64) DUO_LAUNCH((page_append_kernel<64>), grid, dim3(256), s, a);
+    else DUO_LAUNCH((page_append_kernel<128>), grid, dim3(256), s, a);
     return duo_internal_hip_ok(hipGetLastError(), "duo_page_append");
 }
 

@@ -443,7 +443,7 @@ def test_calls_that_do_nothing():
     cache.commit(records)
     assert cache.status.item() == B.PAGE_NO_PLAN and cache.cached.tolist() == [40, 3]
     cache.plan(1)
-    cache._planned = 2
+    cache._batch_c.n_requests = 2  # what the binding keeps a caller from doing
     cache.attention(0, q, out)
     assert cache.status.item() == B.PAGE_NO_PLAN and (out == 9.0).all()
     cache.plan()

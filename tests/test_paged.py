@@ -245,3 +245,13 @@ def test_binding_refuses():
         c.plan(source=B.PageTables(torch.zeros((3, 5), dtype=torch.int32), *c.tables.tensors()[1:]))
     with pytest.raises(ValueError):
         c.set_requests([1] * 4, [0] * 4, [0] * 4)
+    for bad in (torch.zeros((3, 4)), torch.zeros((3, 8), dtype=torch.int32)[:, ::2]):
+        with pytest.raises(ValueError):
+            B.PageTables(bad, *c.tables.tensors()[1:])
+    with pytest.raises(ValueError):
+        c.tables = B.PageTables.empty(2, 4, 10, "cpu")
+    for name in ("cached", "key_pages", "status", "workspace"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(AttributeError):
+        c.tables.held = torch.zeros(3, dtype=torch.int32)
