@@ -54,9 +54,14 @@ struct PagePlanArgs {
     PageLayout lay;
 };
 
-// Exclusive sums of N quantities over the threads of a workgroup of up to 1024, and their totals.
+// Exclusive sums of N quantities over the threads of a workgroup of up to 1024, and their totals: within the waves, then over the waves' totals, which
+// the first lanes of the workgroup sum up, sixteen to a quantity.
 template <int N>
-__device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], int (*lds)[16]) {
+struct PageScan {
+    int wave[16][N], total[N];
+};
+template <int N>
+__device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], PageScan<N>& lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) >> 6;
     int own[N];
 #pragma unroll
@@ -69,47 +74,59 @@ __device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], int (*l
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += lane >= o ? up[i] : 0;
     }
-    __syncthreads();
     if (lane == 63) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) lds[i][wave] = v[i];
+        for (int i = 0; i < N; ++i) lds.wave[wave][i] = v[i];
+    }
+    __syncthreads();
+    if (wave == 0) {
+        for (int j = lane; j < 16 * N; j += 64) {  // 16 lanes a quantity: no quantity is divided between two turns
+            const int w = j & 15, i = j >> 4;
+            int x = w < waves ? lds.wave[w][i] : 0;
+            const int mine = x;
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) {
+                const int up = __shfl_up(x, o, 16);
+                x += w >= o ? up : 0;
+            }
+            if (w == 15) lds.total[i] = x;
+            lds.wave[w][i] = x - mine;
+        }
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        int before = 0, all = 0;
-        for (int w = 0; w < waves; ++w) {
-            const int x = lds[i][w];
-            before += w < wave ? x : 0;
-            all += x;
-        }
-        v[i] += before - own[i];
-        total[i] = all;
+        v[i] += lds.wave[wave][i] - own[i];
+        total[i] = lds.total[i];
     }
 }
 
 // Part one of a plan, one workgroup: checks, sums over the requests, how the attention is cut.  A thread takes PER consecutive requests.
 // What bounds it is the latency of a chain of a dozen dependent steps (loads, two scans, stores).
-constexpr int PAGE_PLAN_THREADS = 1024, PAGE_PLAN_PER = PAGE_MAX_REQUESTS / PAGE_PLAN_THREADS;
+constexpr int PAGE_PLAN_THREADS = 1024;
+struct PageSumLds {
+    PageScan<6> sums;
+    PageScan<5> cuts;
+    int bad;
+};
 
-__global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArgs a) {
-    __shared__ int scan[8][16];
-    __shared__ unsigned long long work[2];
-    __shared__ int bad;
+template <int PER>
+__device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds) {
     PageHeader* const hdr = reinterpret_cast<PageHeader*>(a.ws);
     PageInfo* const info = reinterpret_cast<PageInfo*>(a.ws + a.lay.info);
     const int group = a.hq / a.hkv, page = 1 << a.page_shift, max_slots = a.max_pages << a.page_shift;
     const int per = (a.requests + (int)blockDim.x - 1) / (int)blockDim.x;
-    if (threadIdx.x == 0) work[0] = work[1] = 0, bad = 0;
+    const int F = *a.count_in;
+    if (threadIdx.x == 0) lds.bad = 0;
     __syncthreads();
 
-    PageInfo p[PAGE_PLAN_PER];
+    PageInfo p[PER];
     int wrong = 0;
-    enum { ROWS, REL, TAKE, TILES_S, TILES_B, SUMS };
+    // the attention's work (tiles * blocks) in two halves, whose sums stay inside 32 bits
+    enum { ROWS, REL, TAKE, WORK_S, WORK_T, WORK_T_HIGH, SUMS };
     int sum[SUMS] = {};
-    unsigned long long ws = 0, wt = 0;
 #pragma unroll
-    for (int i = 0; i < PAGE_PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int r = threadIdx.x * per + i;
         p[i] = PageInfo{};
         if (i >= per || r >= a.requests) continue;
@@ -124,40 +141,44 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
         q.need = (q.cached + q.rows + page - 1) >> a.page_shift;
         const PageWork w = page_work(q.cached, q.rows, group);
         q.tiles = w.tiles, q.streamed = w.streamed;
+        const long long work = (long long)w.tiles * w.blocks;
         sum[ROWS] += q.rows;
         sum[REL] += q.held > q.need ? q.held - q.need : 0;
         sum[TAKE] += q.need > q.held ? q.need - q.held : 0;
-        (w.streamed ? ws : wt) += (unsigned long long)w.tiles * w.blocks;
+        sum[WORK_S] += w.streamed ? (int)work : 0;
+        sum[WORK_T] += w.streamed ? 0 : (int)(work & 0xffff);
+        sum[WORK_T_HIGH] += w.streamed ? 0 : (int)(work >> 16);
     }
-    if (wrong) bad = 1;
-    if (ws) atomicAdd(&work[0], ws);  // whole numbers: the order does not matter
-    if (wt) atomicAdd(&work[1], wt);
+    if (wrong) lds.bad = 1;
     int total[SUMS];
-    block_scan(sum, total, scan);  // its barriers stand between the atomics and the reads
-    int status = bad ? DUO_PAGE_BAD_REQUEST : 0;
-    const int F = *a.count_in;
+    block_scan(sum, total, lds.sums);  // its barriers stand between the flag's writes and its read
+    int status = lds.bad ? DUO_PAGE_BAD_REQUEST : 0;
     if (F < 0 || F > a.n_pages || total[ROWS] > a.max_rows || total[REL] > a.n_pages - F) status |= DUO_PAGE_BAD_REQUEST;
     else if (total[TAKE] > F + total[REL]) status |= DUO_PAGE_NO_PAGES;
     const bool ok = status == 0;
 
     // the cuts
     const PageCut few = page_stream_cut(a.max_new, group);
-    const int range_s = page_range((long long)work[0], a.hkv, few.target, few.least);
-    const int range_t = page_range((long long)work[1], a.hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS);
+    const int range_s = page_range(total[WORK_S], a.hkv, few.target, few.least);
+    const int range_t = page_range(((long long)total[WORK_T_HIGH] << 16) + total[WORK_T], a.hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS);
     enum { ITEM_S, ITEM_T, PART_S, PART_T, MERGE, CUTS };
     int cut[CUTS] = {};
 #pragma unroll
-    for (int i = 0; i < PAGE_PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         PageInfo& q = p[i];
         if (q.tiles == 0 || !ok) continue;
-        const int blocks = (q.cached + q.rows + 31) / 32, range = q.streamed ? range_s : range_t;
-        q.chunks = (blocks + range - 1) / range;
+        const int blocks = (q.cached + q.rows + 31) / 32;
+        q.chunks = q.streamed ? page_chunks(blocks, range_s, few.whole) : page_chunks(blocks, range_t, PAGE_TILE_MIN_BLOCKS);
         const int items = q.tiles * q.chunks;
-        cut[q.streamed ? ITEM_S : ITEM_T] += items;
-        if (q.chunks > 1) cut[q.streamed ? PART_S : PART_T] += items, cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
+        cut[ITEM_S] += q.streamed ? items : 0;
+        cut[ITEM_T] += q.streamed ? 0 : items;
+        if (q.chunks == 1) continue;
+        cut[PART_S] += q.streamed ? items : 0;
+        cut[PART_T] += q.streamed ? 0 : items;
+        cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
     }
     int cuts[CUTS];
-    block_scan(cut, cuts, scan);
+    block_scan(cut, cuts, lds.cuts);
 
     if (threadIdx.x == 0) {
         *hdr = PageHeader{PAGE_MAGIC, ok, a.requests, a.hq, a.hkv, a.head_dim, page, a.max_pages, a.max_rows, a.max_new,
@@ -169,7 +190,7 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
         a.row_start[a.requests] = ok ? total[ROWS] : 0;
     }
 #pragma unroll
-    for (int i = 0; i < PAGE_PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int r = threadIdx.x * per + i;
         if (i >= per || r >= a.requests) continue;
         PageInfo& q = p[i];
@@ -185,14 +206,15 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
         sum[REL] += q.held > q.need ? q.held - q.need : 0;
         sum[TAKE] += q.need > q.held ? q.need - q.held : 0;
         const int items = q.tiles * q.chunks;
-        int& at = cut[q.streamed ? ITEM_S : ITEM_T];
-        q.item0 = at;
-        at += items;
+        q.item0 = q.streamed ? cut[ITEM_S] : cut[ITEM_T];
+        cut[ITEM_S] += q.streamed ? items : 0;
+        cut[ITEM_T] += q.streamed ? 0 : items;
         q.part0 = -1;
         if (q.chunks > 1) {
-            int& part = cut[q.streamed ? PART_S : PART_T];
-            q.part0 = part, q.merge0 = cut[MERGE];
-            part += items, cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
+            q.part0 = q.streamed ? cut[PART_S] : cut[PART_T], q.merge0 = cut[MERGE];
+            cut[PART_S] += q.streamed ? items : 0;
+            cut[PART_T] += q.streamed ? 0 : items;
+            cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
         }
         info[r] = q;
         a.held_out[r] = q.need;
@@ -200,8 +222,7 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
     }
 }
 
-// Part two: everything that is as long as rows, pages or items.  blockIdx.x < requests: request blockIdx.x, its threads spread over
-// gridDim.y workgroups; the workgroups beyond copy the free stack and mark the rows behind the last.
+// Part two: everything that is as long as rows, pages or items.
 // In place this is safe: columns that are written ([held, need) of requests that grow) are read by nobody, columns that are read ([need, held)
 // of requests that shrink) are written by nobody, and the stack is read below its old count only and written from there on only.
 __device__ __forceinline__ int released_page(const PagePlanArgs& a, const PageInfo* info, int rank) {
@@ -214,22 +235,20 @@ __device__ __forceinline__ int released_page(const PagePlanArgs& a, const PageIn
     return a.table_in[(size_t)lo * a.max_pages + info[lo].need + (rank - info[lo].rel0)];
 }
 
-__global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
-    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+// The rows behind the last, and the free stack where the tables are not planned in place.
+__device__ __forceinline__ void page_fill_rest(const PagePlanArgs& a, const PageHeader& hdr, int t0, int step) {
+    for (int i = hdr.rows + t0; i < a.max_rows; i += step) a.position[i] = a.slot[i] = -1;
+    if (a.table_out != a.table_in) {
+        const int kept = hdr.ok ? min(hdr.free_in, hdr.free_out) : min(max(*a.count_in, 0), a.n_pages);
+        for (int i = t0; i < kept; i += step) a.free_out[i] = a.free_in[i];
+    }
+}
+
+// One request: its pages, its rows, its part of the attention's schedule.
+__device__ __forceinline__ void page_fill_request(const PagePlanArgs& a, const PageHeader& hdr, int r, int t0, int step) {
     const PageInfo* const info = reinterpret_cast<const PageInfo*>(a.ws + a.lay.info);
     const int group = a.hq / a.hkv;
-    const int t0 = blockIdx.y * blockDim.x + threadIdx.x, step = gridDim.y * blockDim.x;
     const bool copies = a.table_out != a.table_in;
-    if ((int)blockIdx.x >= a.requests) {
-        const int i0 = ((int)blockIdx.x - a.requests) * step + t0, all = ((int)gridDim.x - a.requests) * step;
-        for (int i = hdr.rows + i0; i < a.max_rows; i += all) a.position[i] = a.slot[i] = -1;
-        if (copies) {
-            const int kept = hdr.ok ? min(hdr.free_in, hdr.free_out) : min(max(*a.count_in, 0), a.n_pages);
-            for (int i = i0; i < kept; i += all) a.free_out[i] = a.free_in[i];
-        }
-        return;
-    }
-    const int r = blockIdx.x;
     const int32_t* const line_in = a.table_in + (size_t)r * a.max_pages;
     int32_t* const line = a.table_out + (size_t)r * a.max_pages;
     if (!hdr.ok) {
@@ -292,6 +311,33 @@ __global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
             merge[i] = m;
         }
     }
+}
+
+template <int PER>
+__global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArgs a) {
+    __shared__ PageSumLds lds;
+    page_sum<PER>(a, lds);
+}
+
+// blockIdx.x < requests: request blockIdx.x, its threads spread over gridDim.y workgroups; the workgroups beyond see to the rest.
+__global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
+    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    const int t0 = blockIdx.y * blockDim.x + threadIdx.x, step = gridDim.y * blockDim.x;
+    if ((int)blockIdx.x < a.requests) page_fill_request(a, hdr, blockIdx.x, t0, step);
+    else page_fill_rest(a, hdr, ((int)blockIdx.x - a.requests) * step + t0, ((int)gridDim.x - a.requests) * step);
+}
+
+// Both parts in one workgroup, a wave per request: for steps of up to PAGE_SMALL_REQUESTS requests, PAGE_SMALL_ROWS rows and PAGE_SMALL_PAGES pages,
+// where a second launch is what a plan costs (4 requests: 7.9 us in two launches, 6.2 so).
+constexpr int PAGE_SMALL_REQUESTS = 16, PAGE_SMALL_ROWS = 4096, PAGE_SMALL_PAGES = 16384;
+__global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_plan_kernel(PagePlanArgs a) {
+    __shared__ PageSumLds lds;
+    page_sum<1>(a, lds);
+    __syncthreads();  // what the workgroup has written to memory is there for all of it
+    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (wave < a.requests) page_fill_request(a, hdr, wave, lane, 64);
+    page_fill_rest(a, hdr, threadIdx.x, blockDim.x);
 }
 
 // ---- append

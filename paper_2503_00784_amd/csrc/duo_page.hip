@@ -55,9 +55,12 @@ size_t layer_elems(const duo_model_config* cfg, const duo_page_cache* c) { retur
 template <int D>
 void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStream_t s) {
     constexpr int TEAMS = D == 64 ? 2 : 1;
-    const unsigned few = lay.stream_items * a.hkv;  // more workgroups than the plan has items end at once
+    // Nothing can be cut and every workgroup has a compute unit to itself: eight waves (9 rows of 32 heads behind 512 keys: 7.9 us, 11.4 with four).
+    const bool alone = lay.merges == 0 && a.requests * a.hkv <= 256;
+    const unsigned few = (lay.merges == 0 ? a.requests : lay.stream_items) * a.hkv;  // more workgroups than the plan has items end at once
     if (lay.tile_items > 0) DUO_LAUNCH((page_mixed_kernel<D>), dim3(lay.tile_items * a.hkv + few), dim3(256), s, a);
-    else if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D>), dim3(few), dim3(256), s, a);
+    else if (lay.stream_rows <= 16 && alone) DUO_LAUNCH((page_stream_kernel<D, 8>), dim3(few), dim3(512), s, a);
+    else if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D, 4>), dim3(few), dim3(256), s, a);
     else if (lay.stream_rows <= 32) DUO_LAUNCH((page_team_kernel<D, 1, TEAMS>), dim3(few), dim3(64 * TEAMS), s, a);
     else DUO_LAUNCH((page_team_kernel<D, 2, TEAMS>), dim3(few), dim3(128 * TEAMS), s, a);
     if (lay.merges > 0) {
@@ -100,8 +103,14 @@ extern "C" int duo_page_plan(const duo_model_config* cfg, const duo_page_cache* 
     a.lay = lay;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // not of an earlier call
-    const int threads = b->n_requests >= PAGE_PLAN_THREADS ? PAGE_PLAN_THREADS : (b->n_requests + 63) / 64 * 64;
-    DUO_LAUNCH(page_sum_kernel, dim3(1), dim3(threads), s, a);
+    if (b->n_requests <= PAGE_SMALL_REQUESTS && b->max_rows <= PAGE_SMALL_ROWS && cache->n_pages <= PAGE_SMALL_PAGES) {
+        const int waves = b->n_requests < 4 ? 4 : b->n_requests;
+        DUO_LAUNCH(page_plan_kernel, dim3(1), dim3(64 * waves), s, a);
+        return duo_internal_hip_ok(hipGetLastError(), "duo_page_plan");
+    }
+    static_assert(4 * PAGE_PLAN_THREADS == PAGE_MAX_REQUESTS && PAGE_MAX_REQUESTS == DUO_PAGE_MAX_REQUESTS, "four requests a thread");
+    if (b->n_requests <= PAGE_PLAN_THREADS) DUO_LAUNCH((page_sum_kernel<1>), dim3(1), dim3((b->n_requests + 63) / 64 * 64), s, a);
+    else DUO_LAUNCH((page_sum_kernel<4>), dim3(1), dim3(PAGE_PLAN_THREADS), s, a);
     const int longest = b->max_new > cache->max_pages ? b->max_new : cache->max_pages;
     const int spread = longest > 8192 ? 16 : (longest + 511) / 512;
     const int beyond = (cache->n_pages + 4095) / 4096 / spread + 1;

@@ -149,13 +149,13 @@ __device__ __forceinline__ float decoded(float sum) {  // what the values of a s
 
 // ---- up to 16 rows: the cache's bytes bound the time
 //
-// Four waves, wave w takes blocks w, w + 4, ... of the item.  Keys and values come straight into registers, 1 KiB per load and each byte once: the
+// NW waves, wave w takes blocks w, w + NW, ... of the item.  Keys and values come straight into registers, 1 KiB per load and each byte once: the
 // next block's keys are requested when this block's scores are done, its values when its products are, so a wave always has 8 to 16 KiB
 // in flight and eight waves fit a compute unit.  (Both a whole block ahead: four waves fit, 64 decoding requests 104 -> 115 us.)  The
 // waves' states are joined through LDS.
-template <int D>
-__global__ __launch_bounds__(256) void page_stream_kernel(PageAttnArgs a) {
-    constexpr int KS = D / 32, DT = D / 16, NW = 4;
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void page_stream_kernel(PageAttnArgs a) {
+    constexpr int KS = D / 32, DT = D / 16;
     __shared__ f32x4 lds_o[NW][DT * 64];
     __shared__ float lds_ml[NW][2][16];
     const int index = blockIdx.x / a.hkv, hk = blockIdx.x - index * a.hkv;
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(256) void page_stream_kernel(PageAttnArgs a) {
         }
     }
 
-    // Join the waves: wave w adds its quarter of the channels in wave order.
+    // Join the waves: each adds its part of the channels in wave order.
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (g == 0) lds_ml[wave][0][c] = m, lds_ml[wave][1][c] = l;
@@ -306,8 +306,9 @@ __global__ __launch_bounds__(256) void page_stream_kernel(PageAttnArgs a) {
     }
     const float inv = 1.0f / sum;
 #pragma unroll
-    for (int i = 0; i < DT / NW; ++i) {
-        const int dt = wave * (DT / NW) + i;
+    for (int i = 0; i < (DT + NW - 1) / NW; ++i) {
+        const int dt = wave * ((DT + NW - 1) / NW) + i;
+        if (dt >= DT) break;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) acc += lds_o[w][dt * 64 + lane] * f[w];

@@ -15,11 +15,14 @@ constexpr int PAGE_TILE_ROWS = 128;
 // of more than 16 rows at most: 512 and 16, since their partial results are what a range costs (16 x 33 rows of 32 heads: 81 us, 94 with
 // 1024; 9 rows * 4 behind 30000 keys: 34, 45 with ranges of 32 blocks); of fewer: 1024 and 8 (8 requests behind 1500 keys: 14.4 us, 18.7 with
 // ranges of 32).
+// Requests of up to `whole` blocks are not cut: joining their ranges would cost more (9 rows of 32 heads behind 512 keys: 9.8 us, 10.2 with three ranges
+// and a launch more).
 struct PageCut {
-    int target, least;
+    int target, least, whole;
 };
+__host__ __device__ __forceinline__ int page_chunks(int blocks, int range, int whole) { return blocks <= whole ? 1 : (blocks + range - 1) / range; }
 __host__ __device__ __forceinline__ PageCut page_stream_cut(int max_new, int group) {
-    return (long long)max_new * group <= 16 ? PageCut{1024, 8} : PageCut{512, 16};
+    return (long long)max_new * group <= 16 ? PageCut{1024, 8, 24} : PageCut{512, 16, 24};
 }
 constexpr int PAGE_TILE_TARGET = 512, PAGE_TILE_MIN_BLOCKS = 16;
 
@@ -69,7 +72,7 @@ inline PageLayout page_layout(int requests, int max_rows, int max_new, int max_b
     PageLayout l;
     const PageCut cut = page_stream_cut(max_new, group);
     l.stream_items = cut.target / hkv + requests;
-    l.stream_parts = max_blocks > cut.least ? 2 * cut.target / hkv : 0;
+    l.stream_parts = max_blocks > cut.whole ? 2 * cut.target / hkv : 0;
     // a tiled request has more than PAGE_STREAM_ROWS rows
     const long long all = (long long)max_rows * group;
     const long long tiled_requests = all / (PAGE_STREAM_ROWS + 1) < requests ? all / (PAGE_STREAM_ROWS + 1) : requests;

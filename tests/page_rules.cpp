@@ -27,7 +27,7 @@ void cut(int count, const int* cached, const int* rows, int max_new, int hq, int
     for (int r = 0; r < count; ++r) {
         const PageWork w = page_work(cached[r], rows[r], group);
         if (w.tiles == 0) continue;
-        const int kind = w.streamed ? 0 : 1, chunks = (w.blocks + range[kind] - 1) / range[kind];
+        const int kind = w.streamed ? 0 : 1, chunks = page_chunks(w.blocks, range[kind], kind ? PAGE_TILE_MIN_BLOCKS : few.whole);
         items[kind] += w.tiles * chunks;
         if (chunks > 1) parts[kind] += w.tiles * chunks, merges += page_merge_entries(rows[r] * group, chunks);
         for (int t = 0; t < w.tiles; ++t) {  // the ranges of a tile cover what its rows see, once
