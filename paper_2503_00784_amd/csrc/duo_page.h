@@ -328,8 +328,8 @@ __global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
 }
 
 // Both parts in one workgroup, a wave per request: for steps of up to PAGE_SMALL_REQUESTS requests, PAGE_SMALL_ROWS rows and PAGE_SMALL_PAGES pages,
-// where a second launch is what a plan costs (4 requests: 7.9 us in two launches, 6.2 so).
-constexpr int PAGE_SMALL_REQUESTS = 16, PAGE_SMALL_ROWS = 4096, PAGE_SMALL_PAGES = 16384;
+// where a second launch is what a plan costs (4 requests: 7.9 us in two launches, 6.2 so; 16 requests: 10.9 either way).
+constexpr int PAGE_SMALL_REQUESTS = 8, PAGE_SMALL_ROWS = 4096, PAGE_SMALL_PAGES = 16384;
 __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_plan_kernel(PagePlanArgs a) {
     __shared__ PageSumLds lds;
     page_sum<1>(a, lds);

@@ -349,7 +349,8 @@ struct PageRows {
     float m = -INFINITY, l = 0.f;  // the exponents' reference; this lane's part of the weights' sum
     elem8 qf[KT];
     PageSight sight;
-    int token, gq, last;  // of row `col`; the last slot that any of the 32 rows sees, -1 without a row
+    int token, gq;    // of row `col`
+    int whole, last;  // slots below are seen by all of the 32 rows; the last that any of them sees, -1 without a row
     bool valid;
 
     static __device__ __forceinline__ f32x16 zero() {
@@ -376,6 +377,7 @@ struct PageRows {
         token = pair / group, gq = pair - token * group;
         sight = page_sight(it, token, valid);
         const int here = min(32, it.count - first);
+        whole = it.cached + min((it.first + first) / group + 1, it.trunk);
         last = here > 0 ? it.cached + (it.first + first + here - 1) / group : -1;
         const u16* qp = a.q + (size_t)(it.row0 + token) * a.q_stride + (hk * group + gq) * D + (lane >> 5) * 8;
 #pragma unroll
@@ -573,7 +575,6 @@ __device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, i
     if (nst > 0) request(0);
     Rows rows;
     rows.load(a, it, hk, unit * 32, lane);
-    const int sees_all = it.cached + (it.trunk > 0 ? 1 : 0);  // slots below are seen by every row
     bool odd = false;
     page_queries_landed(rows.qf);
     for (int st = 0; st < nst; ++st) {
@@ -586,7 +587,7 @@ __device__ __forceinline__ void page_team(const PageAttnArgs& a, size_t items, i
         Rows::take_keys(kf, block, lane);
         Rows::take_values(vf, block + KT * 64, lane);
         f32x16 s = rows.scores(kf);
-        if (kb + 32 > sees_all) rows.mask(s, kb, half);
+        if (kb + 32 > rows.whole) rows.mask(s, kb, half);
         Frag8 p[2], lo[2];
         rows.template weigh<true, true>(s, a.scale_log2, p, lo);
         odd |= Rows::clean(vf, it.slots - kb, half);
@@ -696,6 +697,17 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
         for (int i = 0; i < KT / NW; ++i) page_load_lds<false>(k + i * 512, lane * 16, lds_address(lds_k) + ((2 * BPS - 1) * KT + mine + i) * 1024);
         request(0);
     }
+    if (wave * 32 >= it.count) {  // a wave without rows only moves its part of the blocks
+        if (nst > 0) {
+            page_stage_landed<KPW + VPW>();
+            for (int st = 0; st < nst; ++st) {
+                page_stage_landed<0>();
+                request(st + 1);
+            }
+            page_stage_landed<0>();
+        }
+        return;
+    }
     Rows rows;
     rows.load(a, it, hk, wave * 32, lane);
     auto take_keys = [&](elem8 (&f)[KT], int st, int z) { Rows::take_keys(f, lds_k[st & 1] + z * KT * 64, lane); };
@@ -731,15 +743,32 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
             rows.template weigh<false, true>(s1, a.scale_log2, p, p);
             rows.template add<false>(vf, p, p);
         }
-#pragma unroll 1
-        for (int b = whole * BPS; b < nst * BPS; ++b) {
+        // Then what some row does not see: for this wave, blocks that all of its rows see, blocks that some see in part, and the rest, of which it only
+        // moves its share.  Three loops, since a branch around the products would have the outputs copied (to memory, at heads of 128).
+        const int seen_whole = min(max(rows.whole / 32 - it.block0, whole * BPS), it.blocks), seen = min(max(rows.last / 32 + 1 - it.block0, seen_whole), it.blocks);
+        int b = whole * BPS;
+        auto enter = [&] {
             if (b % BPS == 0) {
                 page_stage_landed<0>();
                 request(b / BPS + 1);
             }
+        };
+#pragma unroll 1
+        for (; b < seen_whole; ++b) {
+            enter();
+            Frag8 p[2];
+            rows.template weigh<false, false>(s0, a.scale_log2, p, p);
+            elem8 vf[C32][2];
+            take_values(vf, b / BPS, b % BPS);
+            rows.template add<false>(vf, p, p);
+            s0 = scores_of(b / BPS, b % BPS);
+        }
+#pragma unroll 1
+        for (; b < seen; ++b) {
+            enter();
             int own = half;
             asm volatile("" : "+v"(own));  // keeps what follows from it inside the loop: kept in registers across it, it would push others to memory
-            const int kb = b < it.blocks ? (it.block0 + b) * 32 : 0x40000000;  // behind the range: seen by nobody
+            const int kb = (it.block0 + b) * 32;
             Frag8 p[2];
             rows.mask(s0, kb, own);
             rows.template weigh<false, false>(s0, a.scale_log2, p, p);
@@ -749,6 +778,7 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
             rows.template add<false>(vf, p, p);
             s0 = scores_of(b / BPS, b % BPS);
         }
+        for (; b < nst * BPS; ++b) enter();
         page_stage_landed<0>();  // nothing is in flight to LDS when the workgroup ends
     }
     auto output = [&](int d) {
