@@ -65,7 +65,8 @@ def _check_plan(cache, want, tables):
 
 
 @pytest.mark.parametrize("in_place", [True, False])
-@pytest.mark.parametrize("R,page,seed", [(1, 32, 0), (1, 32, 3), (3, 64, 1), (70, 32, 2), (257, 128, 4), (1100, 32, 5), (4096, 32, 6)])
+@pytest.mark.parametrize("R,page,seed", [(1, 32, 0), (1, 32, 3), (3, 64, 1), (8, 32, 7), (9, 32, 8), (64, 64, 9), (65, 32, 10), (70, 32, 2), (257, 128, 4), (1024, 32, 11),
+                                         (1025, 32, 12), (1100, 32, 5), (4096, 32, 6)])
 def test_plan(R, page, seed, in_place):
     requests, lines, free, n_pages, max_pages = _plan_inputs(R, page, seed)
     if sum(map(U.new_rows, requests)) == 0:
@@ -87,6 +88,17 @@ def test_plan(R, page, seed, in_place):
         for r, line in enumerate(want[3][:50]):
             assert (cache.tables.block_table[r, len(line):] == -7).all()
         assert (cache.tables.free_pages[len(want[5]):] == -7).all()
+
+
+def test_a_plan_of_some_requests_leaves_the_others():
+    """The first 5 of 12 requests: the others keep their pages."""
+    requests, lines, free, n_pages, max_pages = _plan_inputs(12, 32, 21)
+    cache = _planner(requests, lines, free, n_pages, max_pages + 12, 32)
+    want = U.plan(requests[:5], 32, (lines[:5], free), sum(map(U.new_rows, requests)) + 4)
+    cache.plan(5)
+    _check_plan(cache, want, cache.tables)
+    assert cache.tables.held[5:].tolist() == [len(x) for x in lines[5:]]
+    assert [x[:len(y)] for x, y in zip(cache.tables.block_table[5:].tolist(), lines[5:])] == lines[5:]
 
 
 def test_plan_again_changes_nothing():
@@ -291,6 +303,28 @@ def test_attention(step, heads, dtype):
     assert cache.status.item() == 0
 
 
+@pytest.mark.parametrize("rows", [1, 8, 15, 16, 17, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 129, 160, 255, 256, 257])
+@pytest.mark.parametrize("D,cached", [(64, 0), (64, 701), (128, 95), (128, 1500)])
+def test_attention_at_the_sizes_where_the_kernels_change(rows, D, cached):
+    """One request of `rows` rows of one head: short ones in one range, long ones cut."""
+    dtype = "fp16" if rows % 2 else "bf16"
+    requests = [(cached, rows, 0, 0)] if rows % 3 else [(cached, rows - 2 * (rows // 3), 2, rows // 3)]
+    say(rows, D, cached, requests)
+    cache, lines, q, out = _attend(requests, 1, 1, D, dtype, 32, seed=rows)
+    _compare(requests, cache, lines, q, out, 1, 1, D, dtype)
+
+
+@pytest.mark.parametrize("blocks", [1, 7, 8, 9, 16, 17, 23, 24, 25, 31, 32, 33, 64, 65])
+@pytest.mark.parametrize("new", [1, 20, 50, 70])
+def test_attention_at_the_lengths_where_ranges_change(blocks, new):
+    for total in (32 * blocks, 32 * blocks - 1, 32 * blocks + 1):
+        if total < new:
+            continue
+        requests = [(total - new, new, 0, 0)]
+        cache, lines, q, out = _attend(requests, 2, 2, 64, "bf16", 64, seed=blocks)
+        _compare(requests, cache, lines, q, out, 2, 2, 64, "bf16")
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_attention_of_random_steps(seed):
     rng = random.Random(seed)
@@ -313,11 +347,13 @@ def test_attention_scale(scale):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("requests", [[(20, 1, 3, 4)], [(0, 1, 0, 0)], [(70, 60, 2, 25), (5, 1, 0, 0)], [(3000, 1, 2, 2)], [(2500, 80, 0, 0)]])
-def test_what_is_not_seen_does_not_touch_a_row(requests, dtype):
+@pytest.mark.parametrize("requests,D", [([(20, 1, 3, 4)], 128), ([(0, 1, 0, 0)], 128), ([(70, 60, 2, 25), (5, 1, 0, 0)], 128), ([(3000, 1, 2, 2)], 128),
+                                        ([(2500, 80, 0, 0)], 128), ([(40, 3, 4, 6)], 128), ([(1700, 3, 4, 6), (9, 1, 2, 2)], 64), ([(33, 2, 2, 2)], 64),
+                                        ([(130, 2, 3, 4)], 64), ([(100, 40, 3, 30), (7, 1, 1, 2)], 64)])
+def test_what_is_not_seen_does_not_touch_a_row(requests, D, dtype):
     """Slots behind a request's last hold NaN; one branch (or the last trunk row) brings infinities and NaN in keys and values.  Rows that do not see
     it are as if it were not there, rows that do are what the formula gives."""
-    hq, hkv, D, page = 4, 2, 128, 64
+    hq, hkv, page = 4, 2, 64
     t = U.TYPES[dtype]
 
     def poison(cache, lines, q):
