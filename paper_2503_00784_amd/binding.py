@@ -527,6 +527,7 @@ class PagedCache:
         self.device = torch.device(device)
         if self.device.index is None and self.device.type == "cuda":
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = -1 if self.device.type == "cpu" else self.device.index  # as Tensor.get_device has it
         self.lib = load(dtype)
         self.cfg = make_config(shape, 32)
         self.max_requests, self.max_rows = int(max_requests), int(max_rows)
@@ -577,22 +578,21 @@ class PagedCache:
 
     def _call(self, name: str, *args) -> None:
         """The entry point with the cache's device current, on that device's current stream."""
-        torch, function = self.torch, getattr(self.lib, name)
-        index = self.device.index
-        if index == torch.cuda.current_device():
-            rc = function(*args, torch.cuda.current_stream().cuda_stream)
+        cuda, function = self.torch.cuda, getattr(self.lib, name)
+        if self._index == cuda.current_device():
+            rc = function(*args, cuda.current_stream().cuda_stream)
         else:
-            with torch.cuda.device(index):
-                rc = function(*args, torch.cuda.current_stream().cuda_stream)
+            with cuda.device(self._index):
+                rc = function(*args, cuda.current_stream().cuda_stream)
         if rc:
             _check(rc, name)
 
     def _rows(self, name: str, t, heads: int, writes: bool = False):
         """A matrix of the step's rows, [max_rows][heads * head_dim] or [max_rows][heads][head_dim], rows any distance apart: (pointer, distance)."""
         D, shape, stride = self._head_dim, t.shape, t.stride()
-        if t.dtype not in self._element_types or t.device != self.device:
+        if t.dtype not in self._element_types or t.get_device() != self._index:
             raise ValueError(f"{name} must be {self._element_types[0]} or int16 bit patterns on {self.device}, not {t.dtype} on {t.device}")
-        if shape != (self.max_rows, heads * D) and shape != (self.max_rows, heads, D):
+        if shape != (self.max_rows, heads, D) and shape != (self.max_rows, heads * D):
             raise ValueError(f"{name} must be [{self.max_rows}][{heads} * {D}], not {list(shape)}")
         if stride[-1] != 1 or (len(stride) == 3 and heads > 1 and stride[1] != D):
             raise ValueError(f"{name}: the elements of a row must lie together")
@@ -641,9 +641,9 @@ class PagedCache:
     def commit(self, records, cached_out=None) -> None:
         """Enqueue the commit: records int32 [requests][4] as the samplers write them; the new lengths go to `cached`, or to cached_out."""
         out, i32 = self._cached if cached_out is None else cached_out, self.torch.int32
-        if records.dtype != i32 or records.device != self.device or records.shape != (self._planned, 4) or not records.is_contiguous():
+        if records.dtype != i32 or records.get_device() != self._index or records.shape != (self._planned, 4) or not records.is_contiguous():
             raise ValueError(f"records must be contiguous int32 [{self._planned}][4] on {self.device}, not {records.dtype} {list(records.shape)} on {records.device}")
-        if out.dtype != i32 or out.device != self.device or out.dim() != 1 or out.shape[0] < self._planned or not out.is_contiguous():
+        if out.dtype != i32 or out.get_device() != self._index or out.dim() != 1 or out.shape[0] < self._planned or not out.is_contiguous():
             raise ValueError(f"cached_out must be contiguous int32 [{self._planned}] on {self.device}, not {out.dtype} {list(out.shape)} on {out.device}")
         cfg, cache, batch = self._refs
         self._call("duo_page_commit", cfg, cache, self._table_ptr, batch, records.data_ptr(), out.data_ptr(), self._ws_ptr, self.ws_bytes)

@@ -856,13 +856,15 @@ template <int D>
 __global__ __launch_bounds__(256) void page_merge_kernel(PageAttnArgs a) {
     constexpr int E = D / 64, N = PAGE_MERGE_RANGES;
     __shared__ float lds_v[4][D], lds_ml[4][2];
-    const PageHeader* hdr = reinterpret_cast<const PageHeader*>(a.ws);
-    if (!page_plan_is(*hdr, a.requests, a.hq, a.hkv, D, a.page_shift, a.max_pages, a.max_rows, a.max_new)) return;
+    const PageMerge* const merges = reinterpret_cast<const PageMerge*>(a.ws + a.merge);
+    PageMerge mg = merges[blockIdx.x / a.hkv];  // requested with the header; of no meaning behind the last
+    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    if (!page_plan_is(hdr, a.requests, a.hq, a.hkv, D, a.page_shift, a.max_pages, a.max_rows, a.max_new)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.hq / a.hkv;
-    const int units = hdr->merges * a.hkv;  // an entry (some rows of a tile), a head
+    const int units = hdr.merges * a.hkv;  // an entry (some rows of a tile), a head
     for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const int index = unit / a.hkv, hk = unit - index * a.hkv;
-        const PageMerge mg = reinterpret_cast<const PageMerge*>(a.ws + a.merge)[index];
+        if (unit != (int)blockIdx.x) mg = merges[index];
         const int rows = mg.streamed ? a.stream_rows : PAGE_TILE_ROWS;
         const float* part = (mg.streamed ? a.part_stream : a.part_tile) + ((size_t)mg.part0 * a.hkv + hk) * rows * (D + 4);
         const size_t step = (size_t)a.hkv * rows * (D + 4);
