@@ -24,7 +24,9 @@ __host__ __device__ __forceinline__ int page_chunks(int blocks, int range, int w
 __host__ __device__ __forceinline__ PageCut page_stream_cut(int max_new, int group) {
     return (long long)max_new * group <= 16 ? PageCut{1024, 8, 24} : PageCut{512, 16, 24};
 }
-constexpr int PAGE_TILE_TARGET = 512, PAGE_TILE_MIN_BLOCKS = 16;
+// Tiled: one workgroup a compute unit, though two fit there, since a partial result of 128 rows is 67 KB to write and to read again (24 streams
+// beside three chunks of 400 to 1000 rows: 38 us, 43 with 512; 128 rows of 32 heads behind 30000 keys: 25.5 us, 34 with 512 and 31 with 128).
+constexpr int PAGE_TILE_TARGET = 256, PAGE_TILE_MIN_BLOCKS = 16;
 
 // Limits that keep every sum of a plan inside 32 bits: 4096 requests of 2^18 rows, 2^18 pages or 2^18 blocks each.
 constexpr int PAGE_MAX_REQUESTS = 4096, PAGE_MAX_ROWS = 1 << 18, PAGE_MAX_SLOTS = 1 << 23;
