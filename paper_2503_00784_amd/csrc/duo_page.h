@@ -158,8 +158,7 @@ __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds)
     const bool ok = status == 0;
 
     // the cuts
-    const PageCut few = page_stream_cut(a.max_new, group);
-    const int range_s = page_range(total[WORK_S], a.hkv, few.target, few.least);
+    const int range_s = page_stream_range(total[WORK_S], a.hkv, page_stream_cut(a.max_new, group), max_slots >> 5);
     const int range_t = page_range(((long long)total[WORK_T_HIGH] << 16) + total[WORK_T], a.hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS);
     enum { ITEM_S, ITEM_T, PART_S, PART_T, MERGE, CUTS };
     int cut[CUTS] = {};
@@ -168,7 +167,7 @@ __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds)
         PageInfo& q = p[i];
         if (q.tiles == 0 || !ok) continue;
         const int blocks = (q.cached + q.rows + 31) / 32;
-        q.chunks = q.streamed ? page_chunks(blocks, range_s, few.whole) : page_chunks(blocks, range_t, PAGE_TILE_MIN_BLOCKS);
+        q.chunks = page_chunks(blocks, q.streamed ? range_s : range_t);
         const int items = q.tiles * q.chunks;
         cut[ITEM_S] += q.streamed ? items : 0;
         cut[ITEM_T] += q.streamed ? 0 : items;

@@ -12,17 +12,17 @@
 constexpr int PAGE_STREAM_ROWS = 64;
 constexpr int PAGE_TILE_ROWS = 128;
 // Workgroups that the key ranges are cut for (fewer rows and requests than that are split over the keys), and the shortest ranges.  Streamed requests
-// of more than 16 rows at most: 512 and 16, since their partial results are what a range costs (16 x 33 rows of 32 heads: 81 us, 94 with
-// 1024; 9 rows * 4 behind 30000 keys: 34, 45 with ranges of 32 blocks); of fewer: 1024 and 8 (8 requests behind 1500 keys: 14.4 us, 18.7 with
-// ranges of 32).
-// Requests of up to `whole` blocks are not cut: joining their ranges would cost more (9 rows of 32 heads behind 512 keys: 9.8 us, 10.2 with three ranges
-// and a launch more).
+// of more than 16 rows at most: 512 and 4, since their partial results are what a range costs (16 x 33 rows of 32 heads: 80 us, 92 with 1024; 4 x 7 rows
+// * 4 behind 300 to 2000 keys: 15 us, 20 with ranges of 8 blocks or more, 29 with 16); of fewer: 1024 and 8 (8 requests behind 1500 keys: 14 us, 17 with
+// ranges of 4, 19 with 32; 8 x 1 row of 32 heads behind 1000 to 4000: 52, 61 with 512).
+// A batch whose requests have room for `whole` blocks at most is not cut: a second launch that joins ranges would cost more (9 rows of 32 heads behind
+// 512 keys: 8 us, 10 with ranges of 8; 17 rows of 12 heads behind 128: 7 us, 10 with ranges of 4; but 33 rows behind 600: 15 us in ranges of 4, 27 without).  With room for more that launch is there anyway, and short
+// requests are cut like long ones (30 x 1 row behind 100 to 1000 keys: 14 us, 20 uncut).
 struct PageCut {
     int target, least, whole;
 };
-__host__ __device__ __forceinline__ int page_chunks(int blocks, int range, int whole) { return blocks <= whole ? 1 : (blocks + range - 1) / range; }
 __host__ __device__ __forceinline__ PageCut page_stream_cut(int max_new, int group) {
-    return (long long)max_new * group <= 16 ? PageCut{1024, 8, 24} : PageCut{512, 16, 24};
+    return (long long)max_new * group <= 16 ? PageCut{1024, 8, 24} : PageCut{512, 4, 8};
 }
 // Tiled: one workgroup a compute unit, though two fit there, since a partial result of 128 rows is 67 KB to write and to read again (24 streams
 // beside three chunks of 400 to 1000 rows: 38 us, 43 with 512; 128 rows of 32 heads behind 30000 keys: 25.5 us, 34 with 512 and 31 with 128).
@@ -48,6 +48,10 @@ __host__ __device__ __forceinline__ int page_range(long long work, int heads, in
     const long long r = (work * heads + target - 1) / target;
     return r < least ? least : (int)r;
 }
+__host__ __device__ __forceinline__ int page_stream_range(long long work, int heads, const PageCut& cut, int max_blocks) {
+    return max_blocks <= cut.whole ? cut.whole : page_range(work, heads, cut.target, cut.least);
+}
+__host__ __device__ __forceinline__ int page_chunks(int blocks, int range) { return (blocks + range - 1) / range; }
 // A tile that sees `blocks` blocks is cut into at most `chunks` ranges of this length.
 __host__ __device__ __forceinline__ int page_chunk_blocks(int blocks, int chunks) { return (blocks + chunks - 1) / chunks; }
 // Joining the ranges of a tile: a workgroup and head takes this many rows, fewer where a row has many ranges.

@@ -14,20 +14,20 @@ void layout(int requests, int max_rows, int max_new, int max_blocks, int hq, int
 }
 
 // What a plan of these requests (cached, new rows) makes of the attention: items, partial results and merges as the planning kernels count them.
-void cut(int count, const int* cached, const int* rows, int max_new, int hq, int hkv, int* out) {
+void cut(int count, const int* cached, const int* rows, int max_new, int max_blocks, int hq, int hkv, int* out) {
     const int group = hq / hkv;
-    const PageCut few = page_stream_cut(max_new, group);
     long long work[2] = {0, 0};
     for (int r = 0; r < count; ++r) {
         const PageWork w = page_work(cached[r], rows[r], group);
         work[w.streamed ? 0 : 1] += (long long)w.tiles * w.blocks;
     }
-    const int range[2] = {page_range(work[0], hkv, few.target, few.least), page_range(work[1], hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS)};
+    const int range[2] = {page_stream_range(work[0], hkv, page_stream_cut(max_new, group), max_blocks),
+                          page_range(work[1], hkv, PAGE_TILE_TARGET, PAGE_TILE_MIN_BLOCKS)};
     int items[2] = {0, 0}, parts[2] = {0, 0}, merges = 0, covered = 1;
     for (int r = 0; r < count; ++r) {
         const PageWork w = page_work(cached[r], rows[r], group);
         if (w.tiles == 0) continue;
-        const int kind = w.streamed ? 0 : 1, chunks = page_chunks(w.blocks, range[kind], kind ? PAGE_TILE_MIN_BLOCKS : few.whole);
+        const int kind = w.streamed ? 0 : 1, chunks = page_chunks(w.blocks, range[kind]);
         items[kind] += w.tiles * chunks;
         if (chunks > 1) parts[kind] += w.tiles * chunks, merges += page_merge_entries(rows[r] * group, chunks);
         for (int t = 0; t < w.tiles; ++t) {  // the ranges of a tile cover what its rows see, once

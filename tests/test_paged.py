@@ -31,10 +31,10 @@ def _layout(requests, max_rows, max_new, max_blocks, hq, hkv, D):
     return dict(zip(names, out))
 
 
-def _cut(requests, max_new, hq, hkv):
+def _cut(requests, max_new, max_blocks, hq, hkv):
     cached, rows = ((C.c_int * len(requests))(*[r[i] for r in requests]) for i in range(2))
     out = (C.c_int * 6)()
-    rules().cut(len(requests), cached, rows, max_new, hq, hkv, out)
+    rules().cut(len(requests), cached, rows, max_new, max_blocks, hq, hkv, out)
     return dict(zip(("stream_items", "tile_items", "stream_parts", "tile_parts", "merges", "covered"), out))
 
 
@@ -43,7 +43,8 @@ def _fits(requests, hq, hkv, D, max_rows=None, max_new=None, max_slots=None):
     max_rows = max(1, total) if max_rows is None else max_rows
     max_new = max(1, max(r[1] for r in requests)) if max_new is None else max_new
     max_slots = max(32, max(r[0] + r[1] for r in requests)) if max_slots is None else max_slots
-    lay, cut = _layout(len(requests), max_rows, max_new, (max_slots + 31) // 32, hq, hkv, D), _cut(requests, max_new, hq, hkv)
+    max_blocks = (max_slots + 31) // 32
+    lay, cut = _layout(len(requests), max_rows, max_new, max_blocks, hq, hkv, D), _cut(requests, max_new, max_blocks, hq, hkv)
     for name in ("stream_items", "tile_items", "stream_parts", "tile_parts", "merges"):
         assert cut[name] <= lay[name], (name, cut[name], lay[name])
     assert cut["covered"] == 1
