@@ -332,7 +332,7 @@ typedef struct duo_page_cache {
 typedef struct duo_page_tables {
     int32_t *block_table;    /* [n_requests][max_pages]; columns from held[r] on are neither read nor written */
     int32_t *held;           /* [n_requests] pages of the request */
-    int32_t *free_pages;     /* [n_pages] a stack; entries from *free_count on are neither read nor written */
+    int32_t *free_pages;     /* [n_pages] a stack; what a plan finds behind *free_count is not read, and written only up to the new count */
     int32_t *free_count;     /* [1] */
 } duo_page_tables;
 
@@ -349,7 +349,9 @@ typedef struct duo_page_batch {
 
 /* Bytes of workspace of the calls below for this geometry (the fields of batch that count are n_requests, max_rows and
  * max_new; the pointers of cache and batch are not looked at).  duo_page_plan leaves the step's schedule in it, which duo_page_attention
- * and duo_page_commit read: one workspace per step in flight. */
+ * and duo_page_commit read, and attention keeps partial results there: one workspace per step in flight, and the calls on it one after
+ * another.  How the keys are split over workgroups, and with it the order of the sums, follows from the lengths of all requests of the
+ * step, from the batch's maxima and from max_pages * page_slots; equal steps give equal bits. */
 int duo_page_workspace_bytes(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_batch *batch, size_t *bytes);
 
 /*
@@ -358,6 +360,7 @@ int duo_page_workspace_bytes(const duo_model_config *cfg, const duo_page_cache *
  * pages the released ones (requests in order, columns ascending) are pushed behind them; missing pages are popped from
  * that stack in the order in which requests and columns ask for them.  Writes row_start, position, slot and status of the batch and
  * the schedule in the workspace.  `to` may be `from` (in place); otherwise the two share no memory, and `from` is left as it is.
+ * Of tables with more rows than n_requests the rows behind are left alone, in `to` as well.
  */
 int duo_page_plan(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_tables *from, const duo_page_tables *to,
                   const duo_page_batch *batch, void *workspace, size_t workspace_bytes, void *hip_stream);
@@ -366,7 +369,7 @@ int duo_page_plan(const duo_model_config *cfg, const duo_page_cache *cache, cons
  * Rotates queries and keys of max_rows rows to their positions and writes keys and values into the pages of `layer`: q
  * [max_rows][n_q_heads * head_dim], k and v [max_rows][n_kv_heads * head_dim], each with its own distance between rows in elements (a
  * multiple of 8; so they can be column ranges of one projection's output).  q_out as q; it may be q.  Rows whose slot is -1
- * are left out, in q_out too.  Only position, slot, status and max_rows of the batch are read.  The rotation is computed in
+ * are left out, in q_out too; the slots of the others differ.  Only position, slot, status and max_rows of the batch are read.  The rotation is computed in
  * fp32 from angles reduced in double precision, and rounded once.
  */
 int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_batch *batch, int layer,
@@ -378,7 +381,7 @@ int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, co
  * head h / (n_q_heads / n_kv_heads)).  q and out as above; out shares no memory with q; rows of out behind the step's last
  * row are left as they are.  scale > 0, or 0 for 1 / sqrt(head_dim).  Scores, maxima, sums and outputs are fp32; softmax weights
  * enter the second product in the 16-bit type, as pairs (hi + lo) for requests of at most 64 rows * heads of a group,
- * once rounded beyond; the output is rounded once.  What a row does not see does not touch it, infinities and NaN included.
+ * once rounded beyond (weights of less than 2^-126 become zero); the output is rounded once.  What a row does not see does not touch it, infinities and NaN included.
  */
 int duo_page_attention(const duo_model_config *cfg, const duo_page_cache *cache, const int32_t *block_table, const duo_page_batch *batch,
                        int layer, const uint16_t *q, int64_t q_stride, uint16_t *out, int64_t out_stride, float scale,

@@ -578,12 +578,15 @@ class PagedCache:
 
     def _call(self, name: str, *args) -> None:
         """The entry point with the cache's device current, on that device's current stream."""
+        if self._index < 0:
+            raise ValueError(f"{name}: the cache is on {self.device}, the kernels run on a GPU")
         cuda, function = self.torch.cuda, getattr(self.lib, name)
+        stream = self.torch._C._cuda_getCurrentRawStream(self._index)  # the pointer without the Stream object, which costs as much as a launch
         if self._index == cuda.current_device():
-            rc = function(*args, cuda.current_stream().cuda_stream)
+            rc = function(*args, stream)
         else:
             with cuda.device(self._index):
-                rc = function(*args, cuda.current_stream().cuda_stream)
+                rc = function(*args, stream)
         if rc:
             _check(rc, name)
 
@@ -612,7 +615,7 @@ class PagedCache:
 
     def plan(self, n_requests: Optional[int] = None, source: Optional[PageTables] = None) -> None:
         """Enqueue the plan of a step of the first n_requests requests (default: all there is room for).  `source`: the tables to
-        start from, left as they are (`tables` receives the result); default `tables`, in place."""
+        start from, left as they are (`tables` receives the free pages and the rows of the planned requests); default `tables`, in place."""
         n = self.max_requests if n_requests is None else int(n_requests)
         if not 1 <= n <= self.max_requests:
             raise ValueError(f"{n} requests, the cache has room for {self.max_requests}")

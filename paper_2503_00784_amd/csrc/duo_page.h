@@ -357,7 +357,7 @@ struct PageAppendArgs {
 //
 // Rotation: a thread takes eight channels and their eight partners of a row, forms their angles once and goes through the heads: two 16-byte
 // loads and stores each; K's eight channels of a slot are one 16-byte piece of a tile.  The angle is reduced in double precision (position
-// times turns keeps 2^-53 of up to 2^23 positions), sine and cosine of the remainder are fp32.
+// times turns is within 2^-29 turns at 2^23 positions), sine and cosine of the remainder are fp32.
 //
 // Values: a tile holds eight consecutive slots of a channel together.  Eight rows in a row that fill such a piece (all but the ends of a
 // request's rows) are turned around through LDS and written 16 bytes a channel; other rows two bytes a channel.  A workgroup sees to the pieces

@@ -1,6 +1,6 @@
 // Attention of a planned step over the paged cache (see duo_page.h for the plan, duo_page_rules.h for how it is cut).
 //
-// Both kernels form S^T = K Q^T and O^T += V^T P^T with the matrix units on the cache's operand tiles.  A block's key order is such that the
+// All kernels form S^T = K Q^T and O^T += V^T P^T with the matrix units on the cache's operand tiles.  A block's key order is such that the
 // accumulators of S^T are the operand of P^T in the same lane, so nothing crosses lanes between the two products.  The softmax runs online: a
 // row's reference m lags its maximum by up to 2^8, so that weights are at most 2^8, and moves (with the output rescaled) only when a score
 // goes beyond; sums are fp32.
@@ -339,7 +339,6 @@ __device__ __forceinline__ float lane_halves_max(float x) {
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-
 // 32 rows of a wave in 32 x 32 x 16 products.  A lane (col, half) picks its 16 bytes of K and V^T tiles from LDS so that it holds, of row `col`,
 // the scores of eight consecutive keys twice over, which is the operand of the second product.
 template <int D>
@@ -532,7 +531,7 @@ struct PageBlocks {
 // TEAMS teams of UNITS waves, a wave for every 32 rows of the item.  Team z takes blocks z, z + TEAMS, ...: a stage is a block for each team, put in
 // LDS by 16-byte loads from global memory to LDS one stage ahead of its use.  Several workgroups fit a compute unit, so that 64 KiB are in
 // flight and one's start and end go under the other's loads.  The teams' states are joined through LDS.  One team at heads of 128 (32 KiB of LDS
-// a workgroup): 16 x 33 rows of 32 heads 88 us with two, 81 with one; two at heads of 64.
+// a workgroup): 16 x 33 rows of 32 heads 85 us with two, 80 with one (the two launches; 4.7 TB/s); two at heads of 64.
 template <int D, int UNITS, int TEAMS>
 struct PageTeamLds {
     u32x4 kv[2][TEAMS * 2 * PageRows<D>::KT * 64];
@@ -826,8 +825,8 @@ __global__ __launch_bounds__(256, 2) void page_mixed_kernel(PageAttnArgs a) {
 
 // ---- tiles whose keys were cut: the ranges' partial results of a row are joined in their order
 //
-// Up to PAGE_MERGE_RANGES ranges: a wave takes whole rows, several at once, since what it waits for is its loads.  More: the workgroup's four waves take a quarter of the ranges each and the quarters are joined
-// through LDS (a single row behind 131000 keys has 128 ranges: one wave would go through 16 dependent rounds of loads).
+// Up to PAGE_MERGE_RANGES ranges: a wave takes whole rows, several at once, since what it waits for is its loads.  More: the workgroup's four
+// waves take a quarter of the ranges each and the quarters are joined through LDS (a single row behind 131000 keys has 128 ranges: one wave would go through 16 dependent rounds of loads).
 template <int E>
 struct PageJoin {  // a running maximum, sum and output
     float top = -INFINITY, sum = 0.f, acc[E] = {};

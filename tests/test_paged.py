@@ -256,3 +256,13 @@ def test_binding_refuses():
             setattr(c, name, torch.zeros(3, dtype=torch.int32))
     with pytest.raises(AttributeError):
         c.tables.held = torch.zeros(3, dtype=torch.int32)
+
+
+def test_a_cache_on_the_cpu_runs_nothing():
+    torch = pytest.importorskip("torch")
+    shape = inputs.ModelShape(2, 512, 8, 2, 64, 64, 1000)
+    c = B.PagedCache(shape, n_pages=10, max_requests=3, max_pages=4, max_rows=40, max_new=20, device="cpu")
+    q, kv = torch.zeros((40, 8, 64), dtype=torch.bfloat16), torch.zeros((40, 128), dtype=torch.bfloat16)
+    for call in (c.plan, lambda: c.append(0, q, kv, kv), lambda: c.attention(0, q), lambda: c.commit(torch.zeros((3, 4), dtype=torch.int32))):
+        with pytest.raises(ValueError, match="on cpu"):
+            call()
