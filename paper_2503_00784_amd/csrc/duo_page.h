@@ -110,10 +110,19 @@ struct PageSumLds {
     int bad;
 };
 
+// What part two asks of part one: info, header and, in a row of their own, the rel0 of all requests.
+struct PagePlanned {
+    PageHeader* hdr;
+    PageInfo* info;
+    int* released;
+};
+__device__ __forceinline__ PagePlanned page_planned(const PagePlanArgs& a) {
+    return {reinterpret_cast<PageHeader*>(a.ws), reinterpret_cast<PageInfo*>(a.ws + a.lay.info), reinterpret_cast<int*>(a.ws + a.lay.released)};
+}
+
 template <int PER>
 __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds) {
-    PageHeader* const hdr = reinterpret_cast<PageHeader*>(a.ws);
-    PageInfo* const info = reinterpret_cast<PageInfo*>(a.ws + a.lay.info);
+    const PagePlanned out = page_planned(a);
     const int group = a.hq / a.hkv, page = 1 << a.page_shift, max_slots = a.max_pages << a.page_shift;
     const int per = (a.requests + (int)blockDim.x - 1) / (int)blockDim.x;
     const int F = *a.count_in;
@@ -180,9 +189,9 @@ __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds)
     block_scan(cut, cuts, lds.cuts);
 
     if (threadIdx.x == 0) {
-        *hdr = PageHeader{PAGE_MAGIC, ok, a.requests, a.hq, a.hkv, a.head_dim, page, a.max_pages, a.max_rows, a.max_new,
-                          cuts[ITEM_S], cuts[ITEM_T], cuts[MERGE], ok ? total[ROWS] : 0, ok ? F : 0, ok ? F + total[REL] - total[TAKE] : 0,
-                          ok ? total[REL] : 0};
+        *out.hdr = PageHeader{PAGE_MAGIC, ok, a.requests, a.hq, a.hkv, a.head_dim, page, a.max_pages, a.max_rows, a.max_new,
+                              cuts[ITEM_S], cuts[ITEM_T], cuts[MERGE], ok ? total[ROWS] : 0, ok ? F : 0, ok ? F + total[REL] - total[TAKE] : 0,
+                              ok ? total[REL] : 0};
         *a.status = status;
         if (ok) *a.count_out = F + total[REL] - total[TAKE];
         else if (a.count_out != a.count_in) *a.count_out = F;
@@ -197,7 +206,7 @@ __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds)
             if (a.held_out != a.held_in) a.held_out[r] = a.held_in[r];
             a.row_start[r] = 0;
             q = PageInfo{};
-            info[r] = q;
+            out.info[r] = q, out.released[r] = 0;
             continue;
         }
         q.row0 = sum[ROWS], q.rel0 = sum[REL], q.take0 = sum[TAKE];
@@ -215,7 +224,7 @@ __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds)
             cut[PART_T] += q.streamed ? 0 : items;
             cut[MERGE] += page_merge_entries(q.rows * group, q.chunks);
         }
-        info[r] = q;
+        out.info[r] = q, out.released[r] = q.rel0;
         a.held_out[r] = q.need;
         a.row_start[r] = q.row0;
     }
@@ -224,14 +233,15 @@ __device__ __forceinline__ void page_sum(const PagePlanArgs& a, PageSumLds& lds)
 // Part two: everything that is as long as rows, pages or items.
 // In place this is safe: columns that are written ([held, need) of requests that grow) are read by nobody, columns that are read ([need, held)
 // of requests that shrink) are written by nobody, and the stack is read below its old count only and written from there on only.
-__device__ __forceinline__ int released_page(const PagePlanArgs& a, const PageInfo* info, int rank) {
+template <class Released>
+__device__ __forceinline__ int released_page(const PagePlanArgs& a, const PageInfo* info, const Released& released, int rank) {
     int lo = 0, hi = a.requests - 1;  // the last request whose released pages start at or before rank and that has any there
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (info[mid].rel0 <= rank) lo = mid;
+        if (released(mid) <= rank) lo = mid;
         else hi = mid - 1;
     }
-    return a.table_in[(size_t)lo * a.max_pages + info[lo].need + (rank - info[lo].rel0)];
+    return a.table_in[(size_t)lo * a.max_pages + info[lo].need + (rank - released(lo))];
 }
 
 // The rows behind the last, and the free stack where the tables are not planned in place.
@@ -243,9 +253,10 @@ __device__ __forceinline__ void page_fill_rest(const PagePlanArgs& a, const Page
     }
 }
 
-// One request: its pages, its rows, its part of the attention's schedule.
-__device__ __forceinline__ void page_fill_request(const PagePlanArgs& a, const PageHeader& hdr, int r, int t0, int step) {
-    const PageInfo* const info = reinterpret_cast<const PageInfo*>(a.ws + a.lay.info);
+// One request: its pages, its rows, its part of the attention's schedule.  released(i): rel0 of request i.
+template <class Released>
+__device__ __forceinline__ void page_fill_request(const PagePlanArgs& a, const PageHeader& hdr, const PageInfo* info, const Released& released, int r, int t0,
+                                                  int step) {
     const int group = a.hq / a.hkv;
     const bool copies = a.table_out != a.table_in;
     const int32_t* const line_in = a.table_in + (size_t)r * a.max_pages;
@@ -263,7 +274,7 @@ __device__ __forceinline__ void page_fill_request(const PagePlanArgs& a, const P
     auto page_of = [&](int c) {
         if (c < p.held) return line_in[c];
         const int x = top - 1 - (p.take0 + c - p.held);
-        return x < hdr.free_in ? a.free_in[x] : released_page(a, info, x - hdr.free_in);
+        return x < hdr.free_in ? a.free_in[x] : released_page(a, info, released, x - hdr.free_in);
     };
     for (int c = (copies ? 0 : p.held) + t0; c < p.need; c += step) line[c] = page_of(c);
     for (int c = p.need + t0; c < p.held; c += step) {
@@ -318,24 +329,38 @@ __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_sum_kernel(PagePlanArg
     page_sum<PER>(a, lds);
 }
 
-// blockIdx.x < requests: request blockIdx.x, its threads spread over gridDim.y workgroups; the workgroups beyond see to the rest.
+// blockIdx.x < requests: request blockIdx.x, its threads spread over gridDim.y workgroups; the workgroups beyond see to the rest.  Where a request takes
+// pages that others release, the search for whose they are goes through LDS (414
+// requests: 13.0 us for both launches, 12.0 so).
 __global__ __launch_bounds__(256) void page_fill_kernel(PagePlanArgs a) {
-    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    __shared__ int released[PAGE_MAX_REQUESTS];
+    const PagePlanned in = page_planned(a);
+    const PageHeader hdr = *in.hdr;
     const int t0 = blockIdx.y * blockDim.x + threadIdx.x, step = gridDim.y * blockDim.x;
-    if ((int)blockIdx.x < a.requests) page_fill_request(a, hdr, blockIdx.x, t0, step);
-    else page_fill_rest(a, hdr, ((int)blockIdx.x - a.requests) * step + t0, ((int)gridDim.x - a.requests) * step);
+    if ((int)blockIdx.x >= a.requests) {
+        page_fill_rest(a, hdr, ((int)blockIdx.x - a.requests) * step + t0, ((int)gridDim.x - a.requests) * step);
+        return;
+    }
+    const PageInfo p = in.info[blockIdx.x];
+    if (p.need > p.held && hdr.released > 0) {
+        for (int i = threadIdx.x; i < a.requests; i += blockDim.x) released[i] = in.released[i];
+        __syncthreads();
+    }
+    page_fill_request(a, hdr, in.info, [&](int i) { return released[i]; }, blockIdx.x, t0, step);
 }
 
 // Both parts in one workgroup, a wave per request: for steps of up to PAGE_SMALL_REQUESTS requests, PAGE_SMALL_ROWS rows and PAGE_SMALL_PAGES pages,
-// where a second launch is what a plan costs (4 requests: 7.9 us in two launches, 6.2 so; 16 requests: 10.9 either way).
+// where a second launch is what a plan costs (4 requests: 7.2 us in two launches, 6.1 so; 16 requests:
+// 7.4 in two, 9.0).
 constexpr int PAGE_SMALL_REQUESTS = 8, PAGE_SMALL_ROWS = 4096, PAGE_SMALL_PAGES = 16384;
 __global__ __launch_bounds__(PAGE_PLAN_THREADS) void page_plan_kernel(PagePlanArgs a) {
     __shared__ PageSumLds lds;
     page_sum<1>(a, lds);
     __syncthreads();  // what the workgroup has written to memory is there for all of it
-    const PageHeader hdr = *reinterpret_cast<const PageHeader*>(a.ws);
+    const PagePlanned in = page_planned(a);
+    const PageHeader hdr = *in.hdr;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (wave < a.requests) page_fill_request(a, hdr, wave, lane, 64);
+    if (wave < a.requests) page_fill_request(a, hdr, in.info, [&](int i) { return in.info[i].rel0; }, wave, lane, 64);
     page_fill_rest(a, hdr, threadIdx.x, blockDim.x);
 }
 

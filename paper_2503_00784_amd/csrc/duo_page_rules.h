@@ -68,7 +68,7 @@ __host__ __device__ __forceinline__ int page_tile_blocks(int cached, int first, 
 struct PageLayout {
     int stream_items, tile_items, stream_parts, tile_parts, merges;
     int stream_rows;  // rows kept per streamed partial result
-    size_t info, stream, tile, merge, part_stream, part_tile, total;
+    size_t info, released, stream, tile, merge, part_stream, part_tile, total;
 };
 constexpr int PAGE_HEADER_INTS = 64, PAGE_INFO_INTS = 16, PAGE_ITEM_INTS = 16, PAGE_MERGE_INTS = 8;
 
@@ -96,6 +96,7 @@ inline PageLayout page_layout(int requests, int max_rows, int max_new, int max_b
     };
     take(PAGE_HEADER_INTS * 4);
     l.info = take((size_t)requests * PAGE_INFO_INTS * 4);
+    l.released = take((size_t)requests * 4);
     l.stream = take((size_t)l.stream_items * PAGE_ITEM_INTS * 4);
     l.tile = take((size_t)l.tile_items * PAGE_ITEM_INTS * 4);
     l.merge = take((size_t)l.merges * PAGE_MERGE_INTS * 4);
