@@ -325,6 +325,15 @@ def test_attention_at_the_lengths_where_ranges_change(blocks, new):
         _compare(requests, cache, lines, q, out, 2, 2, 64, "bf16")
 
 
+@pytest.mark.parametrize("new", [1, 5, 20])
+@pytest.mark.parametrize("D", [64, 128])
+def test_short_requests_beside_a_long_one(new, D):
+    """The table has room for long requests: short ones are cut too, in the shortest ranges and one block beyond them."""
+    requests = [(2500, 1, 0, 0)] + [(32 * blocks - new + d, new, 0, 0) for blocks in (1, 4, 5, 8, 9, 12, 13, 16, 17) for d in (-1, 0, 1)]
+    cache, lines, q, out = _attend(requests, 2, 1, D, "fp16", 64, seed=new)
+    _compare(requests, cache, lines, q, out, 2, 1, D, "fp16")
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_attention_of_random_steps(seed):
     rng = random.Random(seed)
@@ -643,3 +652,18 @@ def test_other_streams_and_repeats():
         cache.attention(0, q, again[:, :1024])
     stream.synchronize()
     assert torch.equal(out, again)
+
+
+def test_two_caches_on_two_streams():
+    """Steps of two caches enqueued in turn on streams of their own give what each gives alone."""
+    steps = [_attend(STEPS[name], 8, 2, 128, "bf16", 64, seed=i) for i, name in enumerate(("mixed", "long_chunk"))]
+    streams, again = [torch.cuda.Stream() for _ in steps], [torch.full_like(s[3], 9.0) for s in steps]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (cache, _, q, _), stream, out in zip(steps, streams, again):
+            with torch.cuda.stream(stream):
+                cache.plan()
+                cache.attention(0, q, out[:, :1024])
+    torch.cuda.synchronize()
+    for (cache, _, _, out), other in zip(steps, again):
+        assert cache.status.item() == 0 and torch.equal(out, other)
