@@ -65,7 +65,7 @@ void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStre
     else DUO_LAUNCH((page_team_kernel<D, 2, TEAMS>), dim3(few), dim3(128 * TEAMS), s, a);
     if (lay.merges > 0) {
         const long long units = (long long)lay.merges * a.hkv;
-        DUO_LAUNCH((page_merge_kernel<D>), dim3(units < 4096 ? (int)units : 4096), dim3(256), s, a);
+        DUO_LAUNCH((page_merge_kernel<D>), dim3(units < 1024 ? (int)units : 1024), dim3(256), s, a);
     }
 }
 

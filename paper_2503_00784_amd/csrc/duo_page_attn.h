@@ -650,8 +650,8 @@ __global__ __launch_bounds__(64 * TEAMS * UNITS, 2) void page_team_kernel(PageAt
 // Four waves of 32 rows share the keys and values of two blocks (a stage) at a time, put in LDS by 16-byte loads from global memory to LDS.  The
 // scores of a block are formed while the weights of the one before are, so keys run a block ahead of the values: stage st holds the values of
 // blocks 2 st and 2 st + 1 of the range and the keys of 2 st + 1 and 2 st + 2, stage -1 the keys of block 0.  One barrier a stage; two
-// workgroups fit a compute unit, and one's start and end go under the other's products.  Five packed prompts of 900 to 4000 tokens, 32 heads over 8: 185 us,
-// 860 TFLOP/s of the causal half; 1135 in the loop over whole stages (a library product of 8192^3 reaches 1257).
+// workgroups fit a compute unit, and one's start and end go under the other's products.  Five packed prompts of 900 to 4000 tokens, 32 heads over 8: 183 us,
+// 875 TFLOP/s of the causal half; 1135 in the loop over whole stages (a library product of 8192^3 reaches 1257).
 template <int D>
 struct PageTileLds {
     static constexpr int BPS = 2;  // blocks a stage
@@ -678,17 +678,31 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
     const int my_block = wave >> 1, my_tile = (wave & 1) * KPW;  // of a stage
     const uint32_t lds_k_mine = lds_address(lds_k) + (my_block * KT + my_tile) * 1024, lds_v_mine = lds_address(lds_v) + (my_block * DT + my_tile) * 1024;
     int ids_k = 0, ids_v = 0;  // pages of the wave's blocks in stages st .. st + 63
-    auto request = [&](int st) {
+    // A stage's loads go out in four parts, spread over the stage before: a wave that issues all at once stands still for 600 of a stage's 2500 cycles
+    // (16 requests of 132 rows: 56 us so, 53 in parts; the packed prompts 186 and 183).
+    const u16 *next_k = nullptr, *next_v = nullptr;
+    uint32_t next_at = 0;
+    auto request_part = [&](int part) {  // of the stage begun
+#pragma unroll
+        for (int i = 0; i < VPW + KPW; ++i) {
+            if (i * 4 / (VPW + KPW) != part) continue;
+            if (i < VPW) page_load_lds<false>(next_v + i * 512, lane * 16, lds_v_mine + next_at * (BPS * DT * 1024) + i * 1024);
+            else page_load_lds<false>(next_k + (i - VPW) * 512, lane * 16, lds_k_mine + next_at * (BPS * KT * 1024) + (i - VPW) * 1024);
+        }
+    };
+    auto begin = [&](int st) {
         if ((st & 63) == 0) {
             ids_k = where.id((st + lane) * BPS + my_block + 1);
             ids_v = where.id((st + lane) * BPS + my_block);
         }
-        const u16* k = a.kc + where.place<D>(__builtin_amdgcn_readlane(ids_k, st & 63), st * BPS + my_block + 1) + my_tile * 512;
-        const u16* v = a.vc + where.place<D>(__builtin_amdgcn_readlane(ids_v, st & 63), st * BPS + my_block) + my_tile * 512;
+        next_k = a.kc + where.place<D>(__builtin_amdgcn_readlane(ids_k, st & 63), st * BPS + my_block + 1) + my_tile * 512;
+        next_v = a.vc + where.place<D>(__builtin_amdgcn_readlane(ids_v, st & 63), st * BPS + my_block) + my_tile * 512;
+        next_at = st & 1;
+    };
+    auto request = [&](int st) {
+        begin(st);
 #pragma unroll
-        for (int i = 0; i < VPW; ++i) page_load_lds<false>(v + i * 512, lane * 16, lds_v_mine + (st & 1) * (BPS * DT * 1024) + i * 1024);
-#pragma unroll
-        for (int i = 0; i < KPW; ++i) page_load_lds<false>(k + i * 512, lane * 16, lds_k_mine + (st & 1) * (BPS * KT * 1024) + i * 1024);
+        for (int part = 0; part < 4; ++part) request_part(part);
     };
     if (nst > 0) {
         const int mine = wave * (KT / NW);  // block 0's keys are shared out among all four waves
@@ -729,16 +743,20 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
 #pragma unroll 1
         for (; st < whole; ++st) {
             page_stage_landed<0>();  // stage st is there, stage st - 1 drained
-            request(st + 1);
+            begin(st + 1);
             elem8 kf[KT], vf[C32][2];
             Frag8 p[2];
             take_keys(kf, st, 0);
             take_values(vf, st, 0);
+            request_part(0);
             const f32x16 s1 = rows.scores(kf);
+            request_part(1);
             rows.template weigh<false, true>(s0, a.scale_log2, p, p);
+            request_part(2);
             take_keys(kf, st, 1);
             rows.template add<false>(vf, p, p);
             take_values(vf, st, 1);
+            request_part(3);
             s0 = rows.scores(kf);
             rows.template weigh<false, true>(s1, a.scale_log2, p, p);
             rows.template add<false>(vf, p, p);
