@@ -650,8 +650,9 @@ __global__ __launch_bounds__(64 * TEAMS * UNITS, 2) void page_team_kernel(PageAt
 // Four waves of 32 rows share the keys and values of two blocks (a stage) at a time, put in LDS by 16-byte loads from global memory to LDS.  The
 // scores of a block are formed while the weights of the one before are, so keys run a block ahead of the values: stage st holds the values of
 // blocks 2 st and 2 st + 1 of the range and the keys of 2 st + 1 and 2 st + 2, stage -1 the keys of block 0.  One barrier a stage; two
-// workgroups fit a compute unit, and one's start and end go under the other's products.  Five packed prompts of 900 to 4000 tokens, 32 heads over 8: 183 us,
-// 875 TFLOP/s of the causal half; 1135 in the loop over whole stages (a library product of 8192^3 reaches 1257).
+// workgroups fit a compute unit, and one's start and end go under the other's products.  Five packed prompts of 900 to 4000 tokens, 32 heads over 8: 179 us,
+// 895 TFLOP/s of the causal half; 1135 in the loop over whole stages (a library product of 8192^3 reaches 1257).  There two workgroups take 3000 cycles a
+// stage, of which LDS is busy for 2560 (every wave reads the whole stage) and the matrix units for 2048.
 template <int D>
 struct PageTileLds {
     static constexpr int BPS = 2;  // blocks a stage
@@ -679,7 +680,7 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
     const uint32_t lds_k_mine = lds_address(lds_k) + (my_block * KT + my_tile) * 1024, lds_v_mine = lds_address(lds_v) + (my_block * DT + my_tile) * 1024;
     int ids_k = 0, ids_v = 0;  // pages of the wave's blocks in stages st .. st + 63
     // A stage's loads go out in four parts, spread over the stage before: a wave that issues all at once stands still for 600 of a stage's 2500 cycles
-    // (16 requests of 132 rows: 56 us so, 53 in parts; the packed prompts 186 and 183).
+    // (16 requests of 132 rows: 55 us so, 52 in parts; the packed prompts 185 and 179).
     const u16 *next_k = nullptr, *next_v = nullptr;
     uint32_t next_at = 0;
     auto request_part = [&](int part) {  // of the stage begun
