@@ -154,15 +154,20 @@ __device__ __forceinline__ float decoded(float sum) {  // what the values of a s
 // in flight and eight waves fit a compute unit.  The waves' states are joined through LDS.  64 decoding requests, 640 MB: 104 us, 6.1 TB/s; 115
 // with keys and values a whole block ahead, where four waves fit.
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) void page_stream_kernel(PageAttnArgs a) {
+struct PageStreamLds {
+    f32x4 o[NW][D / 16 * 64];
+    float ml[NW][2][16];
+};
+template <int D, int NW>
+__device__ __forceinline__ void page_stream(const PageAttnArgs& a, int place, PageStreamLds<D, NW>& lds) {
     constexpr int KS = D / 32, DT = D / 16;
-    __shared__ f32x4 lds_o[NW][DT * 64];
-    __shared__ float lds_ml[NW][2][16];
-    const int index = blockIdx.x / a.hkv, hk = blockIdx.x - index * a.hkv;
+    auto& lds_o = lds.o;
+    auto& lds_ml = lds.ml;
+    const int index = place / a.hkv, hk = place - index * a.hkv;
     const PageItem it = page_item(reinterpret_cast<const PageItem*>(a.ws + a.stream) + index);  // of no meaning behind the last
     const PageHeader* hdr = reinterpret_cast<const PageHeader*>(a.ws);
     if (!page_plan_is(*hdr, a.requests, a.hq, a.hkv, D, a.page_shift, a.max_pages, a.max_rows, a.max_new)) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, DUO_PAGE_NO_PLAN);
+        if (place == 0 && threadIdx.x == 0) atomicOr(a.status, DUO_PAGE_NO_PLAN);
         return;
     }
     if (index >= hdr->stream_items) return;
@@ -323,6 +328,11 @@ __global__ __launch_bounds__(64 * NW) void page_stream_kernel(PageAttnArgs a) {
             if (dt == 0 && g == 0) dst[D] = top, dst[D + 1] = sum;
         }
     }
+}
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void page_stream_kernel(PageAttnArgs a) {
+    __shared__ PageStreamLds<D, NW> lds;
+    page_stream<D, NW>(a, blockIdx.x, lds);
 }
 
 __device__ __forceinline__ f32x16 mfma32(elem8 a, elem8 b, f32x16 c) {
@@ -831,16 +841,22 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
     if (it.part >= 0 && half == 0) part[D] = rows.m, part[D + 1] = rows.l;
 }
 
-// A step that may hold requests of both kinds: the tiles first, which take longest.
+// A step that may hold requests of every kind: the tiles first, which take longest.
 template <int D>
 __global__ __launch_bounds__(256, 2) void page_mixed_kernel(PageAttnArgs a) {
     __shared__ union Lds {
         PageTileLds<D> tile;
         PageTeamLds<D, 2, 2> team;
+        PageStreamLds<D, 4> stream;
         __device__ Lds() {}
     } lds;
     const int place = (int)blockIdx.x - a.tile_items * a.hkv;
-    if (place < 0) page_tile<D>(a, a.tile, blockIdx.x, lds.tile);
+    if (place < 0) {
+        page_tile<D>(a, a.tile, blockIdx.x, lds.tile);
+        return;
+    }
+    const int rows = __builtin_amdgcn_readfirstlane(reinterpret_cast<const PageItem*>(a.ws + a.stream)[place / a.hkv].count);  // of no meaning behind the last
+    if (rows <= 16) page_stream<D, 4>(a, place, lds.stream);
     else page_team<D, 2, 2>(a, a.stream, place, lds.team);
 }
 
