@@ -660,7 +660,7 @@ __global__ __launch_bounds__(64 * TEAMS * UNITS, 2) void page_team_kernel(PageAt
 // Four waves of 32 rows share the keys and values of two blocks (a stage) at a time, put in LDS by 16-byte loads from global memory to LDS.  The
 // scores of a block are formed while the weights of the one before are, so keys run a block ahead of the values: stage st holds the values of
 // blocks 2 st and 2 st + 1 of the range and the keys of 2 st + 1 and 2 st + 2, stage -1 the keys of block 0.  One barrier a stage; two
-// workgroups fit a compute unit, and one's start and end go under the other's products.  Five packed prompts of 900 to 4000 tokens, 32 heads over 8: 179 us,
+// workgroups fit a compute unit, and one's start and end go under the other's products.  Five packed prompts of 900 to 4000 tokens, 32 heads over 8: 179 us on the better card,
 // 895 TFLOP/s of the causal half; 1135 in the loop over whole stages (a library product of 8192^3 reaches 1257).  There both
 // waves of a SIMD take 1500 cycles a block, of which the matrix unit is busy for 1024 and the vector unit for about 840 (exponentials have a quarter of
 // the rate).
