@@ -524,7 +524,7 @@ __global__ __launch_bounds__(128) void page_commit_kernel(PageCommitArgs a) {
     }
     int moved = 0, after = p.cached + p.trunk;
     if (p.n > 0 && p.k > 0) {
-        if (branch >= p.n || (branch >= 0 && (accepted < 0 || accepted > p.k))) {
+        if (branch < -1 || branch >= p.n || (branch >= 0 && (accepted < 0 || accepted > p.k))) {
             after = p.cached;
             if (first) atomicOr(a.status, DUO_PAGE_BAD_RECORD);
         } else if (branch < 0) {
