@@ -368,8 +368,9 @@ int duo_page_plan(const duo_model_config *cfg, const duo_page_cache *cache, cons
 /*
  * Rotates queries and keys of max_rows rows to their positions and writes keys and values into the pages of `layer`: q
  * [max_rows][n_q_heads * head_dim], k and v [max_rows][n_kv_heads * head_dim], each with its own distance between rows in elements (a
- * multiple of 8; so they can be column ranges of one projection's output).  q_out as q; it may be q.  Rows whose slot is -1
- * are left out, in q_out too; the slots of the others differ.  Only position, slot, status and max_rows of the batch are read.  The rotation is computed in
+ * multiple of 8; so they can be column ranges of one projection's output).  q_out as q; it is q or shares no element with it, and none with
+ * k or v (else DUO_ERR_ARG; column ranges of one matrix, the same distance between rows, are told apart, other matrices by the ranges of their
+ * addresses).  Rows whose slot is -1 are left out, in q_out too; the slots of the others differ.  Only position, slot, status and max_rows of the batch are read.  The rotation is computed in
  * fp32 from angles reduced in double precision, and rounded once.
  */
 int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_batch *batch, int layer,
@@ -378,7 +379,7 @@ int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, co
 
 /*
  * out = softmax(scale q K^T) V of every row of the planned step over what it sees (grouped heads: query head h reads kv
- * head h / (n_q_heads / n_kv_heads)).  q and out as above; out shares no memory with q; rows of out behind the step's last
+ * head h / (n_q_heads / n_kv_heads)).  q and out as above; out shares no element with q (else DUO_ERR_ARG); rows of out behind the step's last
  * row are left as they are.  scale > 0, or 0 for 1 / sqrt(head_dim).  Scores, maxima, sums and outputs are fp32; softmax weights
  * enter the second product in the 16-bit type, as pairs (hi + lo) for requests of at most 64 rows * heads of a group,
  * once rounded beyond (weights of less than 2^-126 become zero); the output is rounded once.  What a row does not see does not touch it, infinities and NaN included.

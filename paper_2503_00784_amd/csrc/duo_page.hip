@@ -50,6 +50,20 @@ int check_rows(const void* p, int64_t stride, int64_t width) {
     return stride < width ? DUO_ERR_SHAPE : DUO_OK;
 }
 
+// Whether two matrices of `rows` rows (start, elements from row to row, elements a row) have an element in common.  Column ranges of one matrix
+// are told apart row by row; matrices with other distances between their rows are taken to meet where their address ranges do.
+bool rows_meet(const uint16_t* a, int64_t a_stride, int64_t a_width, const uint16_t* b, int64_t b_stride, int64_t b_width, int rows) {
+    const __int128 last = rows - 1, delta = ((__int128)(intptr_t)b - (intptr_t)a) / 2;  // both 16-byte aligned
+    if (a_stride != b_stride || rows == 1) return delta < last * a_stride + a_width && delta + last * b_stride + b_width > 0;
+    // row i of b starts delta + d * stride behind row i - d of a: no row is wider than the distance, so two values of d can meet
+    const __int128 d0 = -delta / a_stride;
+    for (__int128 d = d0 - 1; d <= d0 + 1; ++d) {
+        const __int128 at = delta + d * a_stride;
+        if (d >= -last && d <= last && at < a_width && at + b_width > 0) return true;
+    }
+    return false;
+}
+
 size_t layer_elems(const duo_model_config* cfg, const duo_page_cache* c) { return (size_t)c->n_pages * cfg->n_kv_heads * c->page_slots * cfg->head_dim; }
 
 template <int D>
@@ -130,7 +144,9 @@ extern "C" int duo_page_append(const duo_model_config* cfg, const duo_page_cache
     if (const int rc = check_rows(k, k_stride, kd)) return rc;
     if (const int rc = check_rows(v, v_stride, kd)) return rc;
     if (const int rc = check_rows(q_out, q_out_stride, qd)) return rc;
-    if (q_out == q && q_out_stride != q_stride) return DUO_ERR_ARG;
+    // q_out is q or apart from it, and apart from k and v, which other workgroups read while it is written
+    if (q_out == q ? q_out_stride != q_stride : rows_meet(q_out, q_out_stride, qd, q, q_stride, qd, b->max_rows)) return DUO_ERR_ARG;
+    if (rows_meet(q_out, q_out_stride, qd, k, k_stride, kd, b->max_rows) || rows_meet(q_out, q_out_stride, qd, v, v_stride, kd, b->max_rows)) return DUO_ERR_ARG;
     PageAppendArgs a{};
     a.q = q, a.k = k, a.v = v, a.q_out = q_out;
     a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
@@ -167,7 +183,7 @@ extern "C" int duo_page_attention(const duo_model_config* cfg, const duo_page_ca
     const int D = cfg->head_dim, qd = cfg->n_q_heads * D;
     if (const int rc = check_rows(q, q_stride, qd)) return rc;
     if (const int rc = check_rows(out, out_stride, qd)) return rc;
-    if (out == q) return DUO_ERR_ARG;
+    if (rows_meet(out, out_stride, qd, q, q_stride, qd, b->max_rows)) return DUO_ERR_ARG;
     const PageLayout lay = layout_of(cfg, cache, b);
     if (const int rc = check_workspace(lay, workspace, workspace_bytes)) return rc;
     PageAttnArgs a{};
