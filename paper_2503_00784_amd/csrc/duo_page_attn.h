@@ -493,6 +493,15 @@ struct PageRows {
         }
         return any;
     }
+    // Whether an output of any lane's is infinite or not a number: times zero it is not zero.
+    __device__ __forceinline__ bool not_finite_output() const {
+        float sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < C32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum = fmaf(o[d][i], 0.f, sum);
+        return __any(sum != 0.f);
+    }
     // What the values of a block (its tiles in global memory) that are not finite add to channels 32 d .. 32 d + 31 of the rows that see them.
     __device__ __forceinline__ void add_codes(f32x16& x, int d, const u16* tiles, int kb, int keys, int lane) const {
         const int half = lane >> 5;
@@ -811,13 +820,19 @@ __device__ __forceinline__ void page_tile(const PageAttnArgs& a, size_t items, i
         for (; b < nst * BPS; ++b) enter();
         page_stage_landed<0>();  // nothing is in flight to LDS when the workgroup ends
     }
+    // Values that are not finite enter the products of blocks that all rows see as they are, and a weight that rounding made zero makes NaN of an
+    // infinite one.  They leave outputs that are not finite: what the values seen come to replaces those.
+    odd |= rows.not_finite_output();
     auto output = [&](int d) {
         f32x16 x = rows.o[d];
-        if (__builtin_expect(odd, 0)) {  // (in blocks that every row sees whole the product has its way with what is not finite)
-            for (int b = whole * BPS; b < it.blocks; ++b) {
+        if (__builtin_expect(odd, 0)) {
+            f32x16 y = Rows::zero();
+            for (int b = 0; b < it.blocks; ++b) {
                 const int kb = (it.block0 + b) * 32, id = __builtin_amdgcn_readfirstlane(where.id(b));
-                if (kb <= rows.last) rows.add_codes(x, d, a.vc + where.place<D>(id, b), kb, it.slots - kb, lane);
+                if (kb <= rows.last) rows.add_codes(y, d, a.vc + where.place<D>(id, b), kb, it.slots - kb, lane);
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = y[i] == 0.f ? x[i] : y[i];
         }
         return x;
     };
