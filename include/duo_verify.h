@@ -382,8 +382,9 @@ int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, co
  * head h / (n_q_heads / n_kv_heads)).  q and out as above; out shares no element with q (else DUO_ERR_ARG); rows of out behind the step's last
  * row are left as they are.  scale > 0, or 0 for 1 / sqrt(head_dim).  Scores, maxima, sums and outputs are fp32; softmax weights
  * enter the second product in the 16-bit type, as pairs (hi + lo) for requests of at most 64 rows * heads of a group,
- * once rounded beyond (weights of less than 2^-126 become zero); the output is rounded once.  What a row does not see does not touch it, infinities and NaN included;
- * an infinite value or NaN that it sees reaches its channel however small the weight is (down to fp32's least).
+ * once rounded beyond; the output is rounded once.  Weights that the type does not hold become zero, next to a row's largest of 1: below 2^-126
+ * in bf16; below 2^-32 in fp16, where weights of less than 2^-21 are off by up to that.  What a row does not see does not touch it, infinities
+ * and NaN included; an infinite value or NaN that it sees reaches its channel however small the weight is (down to fp32's least).
  */
 int duo_page_attention(const duo_model_config *cfg, const duo_page_cache *cache, const int32_t *block_table, const duo_page_batch *batch,
                        int layer, const uint16_t *q, int64_t q_stride, uint16_t *out, int64_t out_stride, float scale,

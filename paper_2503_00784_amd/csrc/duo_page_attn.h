@@ -2,8 +2,8 @@
 //
 // All kernels form S^T = K Q^T and O^T += V^T P^T with the matrix units on the cache's operand tiles.  A block's key order is such that the
 // accumulators of S^T are the operand of P^T in the same lane, so nothing crosses lanes between the two products.  The softmax runs online: a
-// row's reference m lags its maximum by up to 2^8, so that weights are at most 2^8, and moves (with the output rescaled) only when a score
-// goes beyond; sums are fp32.
+// row's reference m lags its maximum by up to 2^8, so that weights are at most that (raised by 2^7 in fp16, see PAGE_RAISE), and moves (with the
+// output rescaled) only when a score goes beyond; sums are fp32.
 #pragma once
 #include <type_traits>
 
@@ -27,7 +27,16 @@ struct PageAttnArgs {
     float scale_log2;
 };
 
-constexpr float PAGE_LAG = 8.f, PAGE_MOST = 256.f;  // the largest softmax weight and its log2: so far the reference may stay behind
+// How far the reference may stay behind a score, as a log2, and how far the weights are raised on top, so that the 16-bit type holds as small ones as
+// it can: fp16 ends at 2^16 and rounds to zero below 2^-25, which then is 2^-32 of the reference's weight.  Sums and outputs are raised alike, so
+// the factor falls out of their quotient.  (Without it a key in front of a flat tail 2^-25 below lost the tail: 131000 keys, 0.4 % of the sum.)
+#ifdef DUO_FP16
+constexpr float PAGE_LAG = 8.f, PAGE_RAISE = 7.f, PAGE_MOST = 32768.f;  // PAGE_MOST: the largest weight, 2^(lag + raise)
+__device__ __forceinline__ float page_exponent_offset(float ref) { return PAGE_RAISE - ref; }
+#else
+constexpr float PAGE_LAG = 8.f, PAGE_MOST = 256.f;
+__device__ __forceinline__ float page_exponent_offset(float ref) { return -ref; }
+#endif
 
 // What a row sees: slots below `before`, and slots from `lo` to `hi`.
 struct PageSight {
@@ -255,11 +264,11 @@ __device__ __forceinline__ void page_stream(const PageAttnArgs& a, int place, Pa
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
             }
-            const float ref = m == -INFINITY ? 0.f : m;
+            const float offset = page_exponent_offset(m == -INFINITY ? 0.f : m);
             float w[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                w[j] = exp2f(fmaf(s[j], a.scale_log2, -ref));
+                w[j] = exp2f(fmaf(s[j], a.scale_log2, offset));
                 l += w[j];
             }
             Frag8 ph, pl;
@@ -401,19 +410,20 @@ struct PageRows {
         return s;
     }
     // The softmax weights of a block, as operands; l takes their sum.  The row's reference stays where it is while a lane's weights sum to no more
-    // than 2^8, so none of them is larger: no maximum is looked for.  It moves, to the maximum, when they sum to more, and at the first
+    // than PAGE_MOST, so none of them is larger: no maximum is looked for.  It moves, to the maximum, when they sum to more, and at the first
     // block (m = -inf makes infinities or NaN of them).  PAIR: hi and lo parts of the weights, otherwise rounded once.  Not STEADY: the reference follows the
     // maximum at every block, without a branch around the outputs (which cost page_tile<128> copies of them in memory).
     template <bool PAIR, bool STEADY>
     __device__ __forceinline__ void weigh(const f32x16& s, float scale, Frag8 (&p)[2], Frag8 (&lo)[2]) {
         auto with = [&](float ref) {
+            const float offset = page_exponent_offset(ref);
             float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
                 float w[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    w[e] = exp2_raw(fmaf(s[4 * jj + 8 * (e >> 2) + (e & 3)], scale, -ref));
+                    w[e] = exp2_raw(fmaf(s[4 * jj + 8 * (e >> 2) + (e & 3)], scale, offset));
                     sum[e & 1] += w[e];
                 }
                 if (PAIR) {
