@@ -431,7 +431,7 @@ int duo_stream_read_probe(const void *src, size_t bytes, uint32_t *sink, int sin
 /*
  * Per-kernel timing for the roofline report (the per-iteration time breakdown of Sec. 4.4
  * "Profiling", at kernel granularity).  While enabled, every kernel that duo_verify /
- * duo_prefill_chunk launch carries a start and a stop HIP event that take the dispatch's own begin and
+ * duo_prefill_chunk and the duo_page_* calls launch carries a start and a stop HIP event that take the dispatch's own begin and
  * end timestamps; duo_profile_read waits for them, adds each kernel's duration to its class, returns
  * the sums (milliseconds) and launch counts accumulated since the last read, and resets them.
  * Enabling allocates a pool of events, and at most 8192 launches are recorded between two reads (a 64-row step is
@@ -440,18 +440,18 @@ int duo_stream_read_probe(const void *src, size_t bytes, uint32_t *sink, int sin
  * not allocation-free or capturable.  Not thread-safe.
  * ms and launches are HOST arrays of DUO_PROF_CLASSES entries.
  */
-#define DUO_PROF_SETUP     0  /* rotary table, embedding gather + first RMSNorm, input checks, root statistics */
+#define DUO_PROF_SETUP     0  /* rotary table, embedding gather + first RMSNorm, input checks, root statistics; duo_page_plan */
 #define DUO_PROF_QKV       1  /* fused QKV projection + rotary + KV scatter */
-#define DUO_PROF_ATTN      2  /* masked attention over prefix + drafts (chunk partials) */
-#define DUO_PROF_ATTN_COMB 3  /* merge of the chunk partials (long contexts only) */
+#define DUO_PROF_ATTN      2  /* masked attention over prefix + drafts (chunk partials); duo_page_attention */
+#define DUO_PROF_ATTN_COMB 3  /* merge of the chunk partials (long contexts only), of the key ranges in duo_page_attention */
 #define DUO_PROF_OPROJ     4  /* O projection + residual */
 #define DUO_PROF_RESID_REDUCE 5 /* sum of the K-split O/down partial results + residual (more than 16 rows; from 9 rows on where d_ff >= 8192); prompt chunks of more than 80 rows: also the row sums of squares behind an unsplit one */
 #define DUO_PROF_GATEUP    6  /* gate/up projection + SwiGLU */
 #define DUO_PROF_DOWN      7  /* down projection + residual */
 #define DUO_PROF_LMHEAD    8  /* LM head */
 #define DUO_PROF_SAMPLE    9  /* softmax statistics, accept tests, correction/bonus sampling */
-#define DUO_PROF_COMMIT    10 /* sequence selection + KV commit */
-#define DUO_PROF_QKV_FINISH 11 /* 49 rows and more: sum of the K-split Q/K/V partial results + rotary + KV scatter */
+#define DUO_PROF_COMMIT    10 /* sequence selection + KV commit; duo_page_commit */
+#define DUO_PROF_QKV_FINISH 11 /* 49 rows and more: sum of the K-split Q/K/V partial results + rotary + KV scatter; duo_page_append */
 #define DUO_PROF_CLASSES   12
 int duo_profile_enable(int enable);
 int duo_profile_read(double *ms, int32_t *launches);

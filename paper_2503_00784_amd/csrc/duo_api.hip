@@ -36,6 +36,8 @@ constexpr size_t NOALLOC_SCRATCH_BYTES = NOALLOC_STATS_BYTES + NOALLOC_PRUN_BYTE
 static_assert(NOALLOC_SCRATCH_BYTES == DUO_NOALLOC_SCRATCH_BYTES, "the header states the array's size");
 static __device__ __align__(256) unsigned char scratch[NOALLOC_SCRATCH_BYTES];
 
+LaunchEvents g_launch_events;
+
 namespace {
 
 thread_local char g_hip_err[256] = "";
@@ -629,6 +631,7 @@ int spec_sample_on_scratch(const float* logits, const float* root_logits, int vo
 
 int duo_internal_hip_ok(hipError_t e, const char* what) { return hip_ok(e, what); }
 int duo_internal_check_config(const duo_model_config* c) { return check_config(c); }
+void duo_internal_prof(int cls) { prof(cls, nullptr); }
 
 extern "C" {
 

@@ -16,7 +16,8 @@ struct LaunchEvents {
     hipEvent_t start = nullptr, stop = nullptr;
     char* name = nullptr;  // armed: 128 bytes where the launch helper may leave the kernel's name with its template arguments
 };
-static LaunchEvents g_launch_events;
+// one for all of the library's source files (defined in duo_api.hip)
+__attribute__((visibility("hidden"))) extern LaunchEvents g_launch_events;
 // The kernel about to be launched, spelled as a kernel trace prints it (e.g. "gemm_wide_kernel<4, 2, 3, 1, 8, 4, EpiSwiGLU, false>"),
 // so that a timing taken here can be matched with counter summaries taken by a profiler.  No effect unless the timer is armed.
 #define DUO_KERNEL_NAME(...)                                                               \

@@ -72,6 +72,7 @@ void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStre
     // Nothing can be cut and every workgroup has a compute unit to itself: eight waves (9 rows of 32 heads behind 512 keys: 7.9 us, 11.4 with four).
     const bool alone = lay.merges == 0 && a.requests * a.hkv <= 256;
     const unsigned few = (lay.merges == 0 ? a.requests : lay.stream_items) * a.hkv;  // more workgroups than the plan has items end at once
+    duo_internal_prof(DUO_PROF_ATTN);
     if (lay.tile_items > 0) DUO_LAUNCH((page_mixed_kernel<D>), dim3(lay.tile_items * a.hkv + few), dim3(256), s, a);
     else if (lay.stream_rows <= 16 && alone) DUO_LAUNCH((page_stream_kernel<D, 8>), dim3(few), dim3(512), s, a);
     else if (lay.stream_rows <= 16) DUO_LAUNCH((page_stream_kernel<D, 4>), dim3(few), dim3(256), s, a);
@@ -79,6 +80,7 @@ void launch_page_attention(const PageAttnArgs& a, const PageLayout& lay, hipStre
     else DUO_LAUNCH((page_team_kernel<D, 2, TEAMS>), dim3(few), dim3(128 * TEAMS), s, a);
     if (lay.merges > 0) {
         const long long units = (long long)lay.merges * a.hkv;
+        duo_internal_prof(DUO_PROF_ATTN_COMB);
         DUO_LAUNCH((page_merge_kernel<D>), dim3(units < 1024 ? (int)units : 1024), dim3(256), s, a);
     }
 }
@@ -119,15 +121,18 @@ extern "C" int duo_page_plan(const duo_model_config* cfg, const duo_page_cache* 
     (void)hipGetLastError();  // not of an earlier call
     if (b->n_requests <= PAGE_SMALL_REQUESTS && b->max_rows <= PAGE_SMALL_ROWS && cache->n_pages <= PAGE_SMALL_PAGES) {
         const int waves = b->n_requests < 4 ? 4 : b->n_requests;
+        duo_internal_prof(DUO_PROF_SETUP);
         DUO_LAUNCH(page_plan_kernel, dim3(1), dim3(64 * waves), s, a);
         return duo_internal_hip_ok(hipGetLastError(), "duo_page_plan");
     }
     static_assert(4 * PAGE_PLAN_THREADS == PAGE_MAX_REQUESTS && PAGE_MAX_REQUESTS == DUO_PAGE_MAX_REQUESTS, "four requests a thread");
+    duo_internal_prof(DUO_PROF_SETUP);
     if (b->n_requests <= PAGE_PLAN_THREADS) DUO_LAUNCH((page_sum_kernel<1>), dim3(1), dim3((b->n_requests + 63) / 64 * 64), s, a);
     else DUO_LAUNCH((page_sum_kernel<4>), dim3(1), dim3(PAGE_PLAN_THREADS), s, a);
     const int longest = b->max_new > cache->max_pages ? b->max_new : cache->max_pages;
     const int spread = longest > 8192 ? 16 : (longest + 511) / 512;
     const int beyond = (cache->n_pages + 4095) / 4096 / spread + 1;
+    duo_internal_prof(DUO_PROF_SETUP);
     DUO_LAUNCH(page_fill_kernel, dim3(b->n_requests + beyond, spread), dim3(256), s, a);
     return duo_internal_hip_ok(hipGetLastError(), "duo_page_plan");
 }
@@ -168,6 +173,7 @@ extern "C" int duo_page_append(const duo_model_config* cfg, const duo_page_cache
     a.heads_each = each < 1 ? 1 : each > 8 ? 8 : (int)each;
     a.rope_groups = (heads + a.heads_each - 1) / a.heads_each;
     const dim3 grid(windows, a.rope_groups + cfg->n_kv_heads);
+    duo_internal_prof(DUO_PROF_QKV_FINISH);
     if (D == 64) DUO_LAUNCH((page_append_kernel<64>), grid, dim3(256), s, a);
     else DUO_LAUNCH((page_append_kernel<128>), grid, dim3(256), s, a);
     return duo_internal_hip_ok(hipGetLastError(), "duo_page_append");
@@ -220,6 +226,7 @@ extern "C" int duo_page_commit(const duo_model_config* cfg, const duo_page_cache
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // not of an earlier call
     const dim3 grid(b->n_requests, cfg->n_layers, cfg->n_kv_heads);
+    duo_internal_prof(DUO_PROF_COMMIT);
     if (cfg->head_dim == 64) DUO_LAUNCH((page_commit_kernel<64>), grid, dim3(128), s, a);
     else DUO_LAUNCH((page_commit_kernel<128>), grid, dim3(128), s, a);
     return duo_internal_hip_ok(hipGetLastError(), "duo_page_commit");
