@@ -642,7 +642,8 @@ class PagedCache:
         return out
 
     def commit(self, records, cached_out=None) -> None:
-        """Enqueue the commit: records int32 [requests][4] as the samplers write them; the new lengths go to `cached`, or to cached_out."""
+        """Enqueue the commit: records int32 [requests][4] as duo_spec_sample writes them (NoAllocSampler.commit is such a row on the device); the
+        new lengths go to `cached`, or to cached_out."""
         out, i32 = self._cached if cached_out is None else cached_out, self.torch.int32
         if records.dtype != i32 or records.get_device() != self._index or records.shape != (self._planned, 4) or not records.is_contiguous():
             raise ValueError(f"records must be contiguous int32 [{self._planned}][4] on {self.device}, not {records.dtype} {list(records.shape)} on {records.device}")
