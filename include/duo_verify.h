@@ -361,6 +361,9 @@ int duo_page_workspace_bytes(const duo_model_config *cfg, const duo_page_cache *
  * that stack in the order in which requests and columns ask for them.  Writes row_start, position, slot and status of the batch and
  * the schedule in the workspace.  `to` may be `from` (in place); otherwise the two share no memory, and `from` is left as it is.
  * Of tables with more rows than n_requests the rows behind are left alone, in `to` as well.
+ * A request may hold fewer pages than its cached tokens take, one whose keys and values are to be brought back from elsewhere for instance: it is
+ * given pages for those columns too and status stays 0.  What lies in them is the caller's to write in front of the step's attention, which until
+ * then reads what the pages' last owner left there; a caller that brings nothing back has to hold held * page_slots >= cached.
  */
 int duo_page_plan(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_tables *from, const duo_page_tables *to,
                   const duo_page_batch *batch, void *workspace, size_t workspace_bytes, void *hip_stream);

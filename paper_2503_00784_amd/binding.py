@@ -615,7 +615,8 @@ class PagedCache:
 
     def plan(self, n_requests: Optional[int] = None, source: Optional[PageTables] = None) -> None:
         """Enqueue the plan of a step of the first n_requests requests (default: all there is room for).  `source`: the tables to
-        start from, left as they are (`tables` receives the free pages and the rows of the planned requests); default `tables`, in place."""
+        start from, left as they are (`tables` receives the free pages and the rows of the planned requests); default `tables`, in place.
+        A request that holds fewer pages than its cached tokens take gets them here; their keys and values are the caller's to write."""
         n = self.max_requests if n_requests is None else int(n_requests)
         if not 1 <= n <= self.max_requests:
             raise ValueError(f"{n} requests, the cache has room for {self.max_requests}")
