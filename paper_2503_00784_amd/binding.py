@@ -606,12 +606,13 @@ class PagedCache:
 
     def set_requests(self, trunk: Sequence[int], n: Sequence[int], k: Sequence[int], cached: Optional[Sequence[int]] = None) -> None:
         """What the requests bring to the next step, from the host; `cached` only where it is not what the commits left."""
-        for dst, src in ((self._trunk, trunk), (self._n, n), (self._k, k), (self._cached, cached)):
-            if src is not None:
-                src = self.torch.tensor(list(src), dtype=self.torch.int32)
-                if len(src) > self.max_requests:
-                    raise ValueError(f"{len(src)} requests, the cache has room for {self.max_requests}")
-                dst[:len(src)] = src.to(self.device)
+        given = [(dst, self.torch.tensor(list(src), dtype=self.torch.int32))
+                 for dst, src in ((self._trunk, trunk), (self._n, n), (self._k, k), (self._cached, cached)) if src is not None]
+        lengths = [len(src) for _, src in given]
+        if max(lengths) > self.max_requests or min(lengths) != max(lengths):
+            raise ValueError(f"{lengths} requests, the cache has room for {self.max_requests}, and every request brings all of them")
+        for dst, src in given:
+            dst[:len(src)] = src.to(self.device)
 
     def plan(self, n_requests: Optional[int] = None, source: Optional[PageTables] = None) -> None:
         """Enqueue the plan of a step of the first n_requests requests (default: all there is room for).  `source`: the tables to

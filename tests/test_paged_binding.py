@@ -1,0 +1,31 @@
+"""What a refused call of the binding leaves behind: nothing.  Without a GPU."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2503_00784_amd import binding as B
+from paper_2503_00784_amd import inputs
+
+
+@pytest.fixture
+def cache():
+    return B.PagedCache(inputs.ModelShape(2, 512, 8, 2, 64, 64, 1000), n_pages=10, max_requests=3, max_pages=4, max_rows=40, max_new=20, device="cpu")
+
+
+@pytest.mark.parametrize("lists", [([7, 7, 7], [5, 5, 5, 5], [6, 6, 6], None), ([7, 7, 7], [5, 5, 5], [6, 6, 6], [9] * 4), ([7, 7], [5], [6, 6], None),
+                                   ([7, 7, 7], [], [6, 6, 6], None), ([7], [5], [6, 6], None), ([7, 7], [5, 5], [6, 6], [9]), ([7, 7, 7], [5, 5, 5], [1 << 40] * 3, None),
+                                   ([7, 7, 7], [5, 5, 5], [6, 6, "x"], None)])
+def test_requests_are_set_whole_or_not_at_all(cache, lists):
+    """Lists of other lengths, or too long, or of other things: no request keeps the branches of one step and the trunk of another."""
+    cache.set_requests([1, 2, 3], [4, 0, 1], [2, 0, 3], [30, 31, 32])
+    with pytest.raises((ValueError, RuntimeError, TypeError)):
+        cache.set_requests(*lists)
+    assert [x.tolist() for x in (cache.trunk, cache.n, cache.k, cache.cached)] == [[1, 2, 3], [4, 0, 1], [2, 0, 3], [30, 31, 32]]
+
+
+def test_requests_that_are_set(cache):
+    cache.set_requests([1, 2, 3], [4, 0, 1], [2, 0, 3], [30, 31, 32])
+    cache.set_requests((5, 6), iter((0, 2)), [1, 1])  # the first two; what is cached stays
+    assert [x.tolist() for x in (cache.trunk, cache.n, cache.k, cache.cached)] == [[5, 6, 3], [0, 2, 1], [1, 1, 3], [30, 31, 32]]
+    cache.set_requests([], [], [])
+    assert cache.trunk.tolist() == [5, 6, 3]
