@@ -623,8 +623,12 @@ class PagedCache:
             raise ValueError(f"{n} requests, the cache has room for {self.max_requests}")
         src = self._tables_ref if source is None else C.byref(self._fits(source).c)
         cfg, cache, batch = self._refs
-        self._batch_c.n_requests = self._planned = n
-        self._call("duo_page_plan", cfg, cache, src, self._tables_ref, batch, self._ws_ptr, self.ws_bytes)
+        self._batch_c.n_requests = n
+        try:
+            self._call("duo_page_plan", cfg, cache, src, self._tables_ref, batch, self._ws_ptr, self.ws_bytes)
+            self._planned = n
+        finally:
+            self._batch_c.n_requests = self._planned  # of the plan before, where this one was not enqueued
 
     def append(self, layer: int, q, k, v, q_out=None):
         """Enqueue the rotary embedding of q and k and the writing of k and v into the pages; returns q_out (default: in place)."""

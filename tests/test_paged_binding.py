@@ -29,3 +29,29 @@ def test_requests_that_are_set(cache):
     assert [x.tolist() for x in (cache.trunk, cache.n, cache.k, cache.cached)] == [[5, 6, 3], [0, 2, 1], [1, 1, 3], [30, 31, 32]]
     cache.set_requests([], [], [])
     assert cache.trunk.tolist() == [5, 6, 3]
+
+
+def test_a_plan_that_is_not_enqueued_leaves_the_one_before(cache):
+    """The calls behind it still belong to a step of the requests planned last."""
+    with pytest.raises(ValueError, match="on cpu"):
+        cache.plan(2)
+    with pytest.raises(ValueError, match="on cpu"):
+        cache.commit(torch.zeros((3, 4), dtype=torch.int32))
+    with pytest.raises(ValueError, match="records"):
+        cache.commit(torch.zeros((2, 4), dtype=torch.int32))
+
+
+@pytest.mark.gpu
+def test_a_refused_plan_leaves_the_step_before():
+    """Tables that are in place in part are refused; attention and commit of the planned step go on."""
+    import paged_util as U
+    cache, _ = U.make([(40, 1, 0, 0), (3, 5, 0, 0)], 4, 2, 64, "bf16", 32)
+    q = torch.randn((cache.max_rows, 4, 64), device="cuda:0").bfloat16()
+    cache.plan()
+    want = cache.attention(0, q).clone()
+    block_table, *others = cache.tables.tensors()
+    with pytest.raises(B.DuoError):
+        cache.plan(1, source=B.PageTables(block_table.clone(), *others))
+    assert torch.equal(cache.attention(0, q), want) and cache.status.item() == 0
+    cache.commit(torch.tensor([[-1, 0, 1, 0]] * 2, dtype=torch.int32, device="cuda:0"))
+    assert cache.cached.tolist() == [41, 8] and cache.status.item() == 0
