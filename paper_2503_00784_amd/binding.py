@@ -528,6 +528,8 @@ class PagedCache:
         if self.device.index is None and self.device.type == "cuda":
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = -1 if self.device.type == "cpu" else self.device.index  # as Tensor.get_device has it
+        # the current stream's pointer without a Stream object, which costs as much as a launch, where torch has that (it is no public name)
+        self._stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         self.lib = load(dtype)
         self.cfg = make_config(shape, 32)
         self.max_requests, self.max_rows = int(max_requests), int(max_rows)
@@ -581,7 +583,7 @@ class PagedCache:
         if self._index < 0:
             raise ValueError(f"{name}: the cache is on {self.device}, the kernels run on a GPU")
         cuda, function = self.torch.cuda, getattr(self.lib, name)
-        stream = self.torch._C._cuda_getCurrentRawStream(self._index)  # the pointer without the Stream object, which costs as much as a launch
+        stream = self._stream_of(self._index)
         if self._index == cuda.current_device():
             rc = function(*args, stream)
         else:

@@ -55,3 +55,29 @@ def test_a_refused_plan_leaves_the_step_before():
     assert torch.equal(cache.attention(0, q), want) and cache.status.item() == 0
     cache.commit(torch.tensor([[-1, 0, 1, 0]] * 2, dtype=torch.int32, device="cuda:0"))
     assert cache.cached.tolist() == [41, 8] and cache.status.item() == 0
+
+
+@pytest.mark.gpu
+def test_streams_without_the_short_way_to_them(monkeypatch):
+    """The public call names the same stream: a step's calls on a stream of their own, in order behind what that stream does before."""
+    import paged_util as U
+
+    def outputs():
+        cache, _ = U.make([(40, 1, 0, 0), (3, 5, 0, 0)], 4, 2, 64, "bf16", 32)
+        q = torch.randn((cache.max_rows, 4, 64), generator=torch.Generator(device="cuda:0").manual_seed(1), device="cuda:0").bfloat16()
+        stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            assert cache._stream_of(0) == stream.cuda_stream
+            late = torch.zeros_like(q)
+            for _ in range(50):
+                late.copy_(q)
+            cache.plan()
+            out = cache.attention(0, late)
+        stream.synchronize()
+        assert cache.status.item() == 0
+        return out
+
+    want = outputs()
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert torch.equal(outputs(), want)
