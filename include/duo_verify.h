@@ -373,8 +373,8 @@ int duo_page_plan(const duo_model_config *cfg, const duo_page_cache *cache, cons
  * [max_rows][n_q_heads * head_dim], k and v [max_rows][n_kv_heads * head_dim], each with its own distance between rows in elements (a
  * multiple of 8; so they can be column ranges of one projection's output).  q_out as q; it is q or shares no element with it, and none with
  * k or v (else DUO_ERR_ARG; column ranges of one matrix, the same distance between rows, are told apart, other matrices by the ranges of their
- * addresses).  Rows whose slot is -1 are left out, in q_out too; the slots of the others differ.  Only position, slot, status and max_rows of the batch are read.  The rotation is computed in
- * fp32 from angles reduced in double precision, and rounded once.
+ * addresses).  Rows whose slot is -1 are left out, in q_out too; the slots of the others differ.  Only position, slot, status and max_rows of the
+ * batch are read.  The rotation is computed in fp32 from angles reduced in double precision, and rounded once.
  */
 int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, const duo_page_batch *batch, int layer,
                     const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
@@ -388,6 +388,7 @@ int duo_page_append(const duo_model_config *cfg, const duo_page_cache *cache, co
  * once rounded beyond; the output is rounded once.  Weights that the type does not hold become zero, next to a row's largest of 1: below 2^-126
  * in bf16; below 2^-32 in fp16, where weights of less than 2^-21 are off by up to that.  What a row does not see does not touch it, infinities
  * and NaN included; an infinite value or NaN that it sees reaches its channel however small the weight is (down to fp32's least).
+ * The fp32 sums are divided at the end: values whose sum under weights of up to 2^8 is beyond fp32 (bf16 values of 2^100 and more) may give infinity.
  */
 int duo_page_attention(const duo_model_config *cfg, const duo_page_cache *cache, const int32_t *block_table, const duo_page_batch *batch,
                        int layer, const uint16_t *q, int64_t q_stride, uint16_t *out, int64_t out_stride, float scale,

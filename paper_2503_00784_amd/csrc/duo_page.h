@@ -388,8 +388,9 @@ struct PageAppendArgs {
 // request's rows) are turned around through LDS and written 16 bytes a channel; other rows two bytes a channel.  A workgroup sees to the pieces
 // that start in its rows, so it reads up to seven rows more.
 //
-// 8410 rows of 32 query and 8 key heads of 128: 35 us (5.8 TB/s of what is read and written once; a copy reaches 4.9); 80 with a sine and cosine for
-// every head and two bytes a channel throughout.
+// 8410 rows of 32 query and 8 key heads of 128: 50 us from cold caches (4.1 TB/s of what is read and written once; a copy of 2 GiB reaches 4.9), 35
+// where the last-level cache still holds the rows, as behind the projection that wrote them; 80 there with a sine and cosine for every head and two
+// bytes a channel throughout.
 constexpr int PAGE_APPEND_ROWS = 32;
 
 template <int D>

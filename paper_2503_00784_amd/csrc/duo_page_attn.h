@@ -411,8 +411,12 @@ struct PageRows {
     }
     // The softmax weights of a block, as operands; l takes their sum.  The row's reference stays where it is while a lane's weights sum to no more
     // than PAGE_MOST, so none of them is larger: no maximum is looked for.  It moves, to the maximum, when they sum to more, and at the first
-    // block (m = -inf makes infinities or NaN of them).  PAIR: hi and lo parts of the weights, otherwise rounded once.  Not STEADY: the reference follows the
-    // maximum at every block, without a branch around the outputs (which cost page_tile<128> copies of them in memory).
+    // block (m = -inf makes infinities or NaN of them).  PAIR: hi and lo parts of the weights, otherwise rounded once: in tiles, which the matrix units
+    // bound.  There it makes the root-mean-square error against 64 bits 1.3 times that of the output's own rounding (relative: bf16 0.0021 next to
+    // 0.0016, fp16 2.6e-4 next to 2.1e-4); pairs leave the latter alone and cost half as many products again: packed prompts 239 us instead of 184, chunks 40
+    // instead of 35.
+    // Not STEADY: the reference follows the maximum at every block, without a branch around the outputs (which cost page_tile<128> copies of them in
+    // memory).
     template <bool PAIR, bool STEADY>
     __device__ __forceinline__ void weigh(const f32x16& s, float scale, Frag8 (&p)[2], Frag8 (&lo)[2]) {
         auto with = [&](float ref) {

@@ -15,17 +15,24 @@ constexpr int PAGE_TILE_ROWS = 128;
 // of more than 16 rows at most: 512 and 4, since their partial results are what a range costs (16 x 33 rows of 32 heads: 80 us, 92 with 1024; 4 x 7 rows
 // * 4 behind 300 to 2000 keys: 15 us, 20 with ranges of 8 blocks or more, 29 with 16); of fewer: 1024 and 8 (8 requests behind 1500 keys: 14 us, 17 with
 // ranges of 4, 19 with 32; 8 x 1 row of 32 heads behind 1000 to 4000: 52, 61 with 512).
-// A batch whose requests have room for `whole` blocks at most is not cut: a second launch that joins ranges would cost more (9 rows of 32 heads behind
-// 512 keys: 8 us, 10 with ranges of 8; 17 rows of 12 heads behind 128: 7 us, 10 with ranges of 4; but 33 rows behind 600: 15 us in ranges of 4, 27 without).  With room for more that launch is there anyway, and short
-// requests are cut like long ones (30 x 1 row behind 100 to 1000 keys: 14 us, 20 uncut).
+// A batch whose requests have room for `whole` blocks at most is not cut, since a second launch joins ranges.  Uncut against cut, replayed graphs, us:
+//   up to 16 rows, 9 rows of 32 heads behind 100, 512, 750, 1000 and 2000 keys: 5.3 7.9 9.8 12.4 21.0 against 7.0 9.9 10.0 10.4 12.0; 8 requests of
+//   one row, 32 heads over 8: 5.2 8.9 10.3 13.4 23.3 against 7.2 9.6 10.0 10.4 15.5: they cross at about 24 blocks;
+//   more rows, 33 of 32 heads behind 100, 200, 300 and 512: 10.9 14.4 17.6 25.1 against 11.3 13.2 13.1 14.3; 17 of 12 heads of 64: 5.9 7.4 8.2 11.3
+//   against 7.5 9.2 9.2 10.5: between 4 and 12 blocks.
+// (Steps whose workgroups fill the card uncut do not need ranges at any length: 8 x 9 rows of 32 heads behind 2000 keys 43 against 49.)
+// Short requests in a table with room for more are cut all the same: the joining launch is there anyway, and what it costs them is the difference
+// above (2 us at 512 keys).  With it, ranges are the faster form (30 x 1 row behind 100 to 1000 keys: 14 us, 20 in whole ranges).
 struct PageCut {
     int target, least, whole;
 };
 __host__ __device__ __forceinline__ PageCut page_stream_cut(int max_new, int group) {
     return (long long)max_new * group <= 16 ? PageCut{1024, 8, 24} : PageCut{512, 4, 8};
 }
-// Tiled: one workgroup a compute unit, though two fit there, since a partial result of 128 rows is 67 KB to write and to read again (24 streams
-// beside three chunks of 400 to 1000 rows: 38 us, 43 with 512; 128 rows of 32 heads behind 30000 keys: 25.5 us, 34 with 512 and 31 with 128).
+// Tiled: one workgroup a compute unit, though two fit there at heads of 128 and three at 64, since a partial result of 128 rows is 67 or 35 KB to
+// write and to read again.  With 256, 512 and 128, replayed graphs: 24 streams beside three chunks of 400 to 1000 rows, heads of 64: 37, 42, 36 us;
+// 128 rows of 32 heads behind 30000 keys: 27, 37, 31; 512 rows of 32 heads behind 3000: 28.5, 30.5, 29.4; 64 decoding requests beside a chunk of 512
+// rows: 135, 149, 122 (there the streams want the card).
 constexpr int PAGE_TILE_TARGET = 256, PAGE_TILE_MIN_BLOCKS = 16;
 
 // Limits that keep every sum of a plan inside 32 bits: 4096 requests of 2^18 rows, 2^18 pages or 2^18 blocks each.
