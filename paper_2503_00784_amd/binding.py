@@ -27,6 +27,8 @@ PAGE_NO_PAGES, PAGE_BAD_REQUEST, PAGE_BAD_PAGE, PAGE_NO_PLAN, PAGE_BAD_RECORD = 
 PAGE_MAX_REQUESTS = 4096
 PAGE_MAX_ROWS = 262144
 PAGE_MAX_SLOTS = 8388608
+SCALED_MAX_N, SCALED_MAX_K, SCALED_MAX_ROWS = 1048576, 65536, 262144
+MOE_MAX_EXPERTS, MOE_MAX_TOP = 512, 16
 
 EXPORTS = ["duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample_workspace_bytes",
            "duo_spec_sample", "duo_spec_sample_noalloc", "duo_verify_deferred", "duo_deferred_sample", "duo_skinny_gemm",
@@ -34,10 +36,12 @@ EXPORTS = ["duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample
            "duo_v_cache_offset", "duo_status_string", "duo_last_hip_error", "duo_profile_enable",
            "duo_profile_read", "duo_profile_dropped", "duo_profile_kernel_name", "duo_packed_elems", "duo_pack_matrix", "duo_pack_qkv", "duo_pack_gate_up",
            "duo_pack_activations",
-           "duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit"]
+           "duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit",
+           "duo_scaled_bytes", "duo_scaled_pack", "duo_scaled_workspace_bytes", "duo_scaled_gemm",
+           "duo_moe_expert_bytes", "duo_moe_pack", "duo_moe_workspace_bytes", "duo_moe_layer"]
 NOALLOC_MAX_VOCAB = 131072
 PROF_CLASSES = ["setup", "qkv_rope", "attn", "attn_combine", "o_proj", "residual_reduce", "gate_up_swiglu", "down_proj", "lm_head",
-                "sample", "commit", "qkv_finish"]
+                "sample", "commit", "qkv_finish", "scaled_gemm", "moe_router", "moe_gate_up", "moe_down"]
 
 _u16p = C.POINTER(C.c_uint16)
 _u16pp = C.POINTER(_u16p)
@@ -79,6 +83,10 @@ class PageTablesC(C.Structure):
 class PageBatchC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("cached", "trunk", "n", "k", "row_start", "position", "slot", "status")] + \
                [(n, C.c_int32) for n in ("n_requests", "max_rows", "max_new")]
+
+
+class MoeConfigC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("d_model", "d_ff", "n_experts", "top_k", "scaled", "renormalise")]
 
 
 class DuoError(RuntimeError):
@@ -149,7 +157,20 @@ def load(dtype: str = "bf16") -> C.CDLL:
     lib.duo_page_attention.argtypes = page + [C.c_void_p, C.POINTER(PageBatchC), C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_float,
                                               C.c_void_p, C.c_size_t, C.c_void_p]
     lib.duo_page_commit.argtypes = page + [C.c_void_p, C.POINTER(PageBatchC), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
-    for name in ("duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit",
+    lib.duo_scaled_bytes.argtypes = [C.c_int, C.c_int]
+    lib.duo_scaled_pack.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
+    lib.duo_scaled_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+    lib.duo_scaled_gemm.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t,
+                                    C.c_void_p]
+    lib.duo_moe_expert_bytes.argtypes = [C.POINTER(MoeConfigC)]
+    lib.duo_moe_pack.argtypes = [C.POINTER(MoeConfigC), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+    lib.duo_moe_workspace_bytes.argtypes = [C.POINTER(MoeConfigC), C.c_int, C.POINTER(C.c_size_t)]
+    lib.duo_moe_layer.argtypes = [C.POINTER(MoeConfigC), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    for name in ("duo_scaled_bytes", "duo_moe_expert_bytes"):
+        getattr(lib, name).restype = C.c_size_t
+    for name in ("duo_scaled_pack", "duo_scaled_workspace_bytes", "duo_scaled_gemm", "duo_moe_pack", "duo_moe_workspace_bytes", "duo_moe_layer",
+                 "duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit",
                  "duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample_workspace_bytes",
                  "duo_spec_sample", "duo_verify_deferred", "duo_deferred_sample", "duo_skinny_gemm", "duo_block_gemm", "duo_pack_matrix",
                  "duo_pack_qkv", "duo_pack_gate_up", "duo_pack_activations"):
@@ -659,6 +680,200 @@ class PagedCache:
             raise ValueError(f"cached_out must be contiguous int32 [{self._planned}] on {self.device}, not {out.dtype} {list(out.shape)} on {out.device}")
         cfg, cache, batch = self._refs
         self._call("duo_page_commit", cfg, cache, self._table_ptr, batch, records.data_ptr(), out.data_ptr(), self._ws_ptr, self.ws_bytes)
+
+
+class _OnDevice:
+    """A handle whose calls go to the current stream of its own device, whatever device is current."""
+
+    def _settle(self, device, dtype: str) -> None:
+        import torch
+        self._torch = torch
+        self.device, self.dtype = torch.device(device), dtype
+        if self.device.type != "cuda":
+            raise ValueError(f"the kernels run on a GPU, not on {self.device}")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        self._element = torch.float16 if dtype == "fp16" else torch.bfloat16
+        # the current stream's pointer without a Stream object, where torch has that (it is no public name)
+        self._stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self.lib = load(dtype)
+
+    def _call(self, name: str, *args) -> None:
+        cuda, function = self._torch.cuda, getattr(self.lib, name)
+        stream = self._stream_of(self._index)
+        if self._index == cuda.current_device():
+            rc = function(*args, stream)
+        else:
+            with cuda.device(self._index):
+                rc = function(*args, stream)
+        if rc:
+            _check(rc, name)
+
+    def _matrix(self, name: str, w, N: int, K: int):
+        """A weight matrix as the packing calls take it: contiguous, of the handle's type, 16-byte aligned."""
+        if tuple(w.shape) != (N, K) or w.dtype != self._element or w.get_device() != self._index:
+            raise ValueError(f"{name} must be {self._element} [{N}][{K}] on {self.device}, not {w.dtype} {list(w.shape)} on {w.device}")
+        w = w.contiguous()
+        return w if w.data_ptr() % 16 == 0 else w.clone()
+
+    def _rows(self, name: str, t, width: int, types, writes: bool = False):
+        """(pointer, rows, elements from row to row) of a matrix of rows."""
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 2 or shape[1] != width or t.dtype not in types or t.get_device() != self._index:
+            raise ValueError(f"{name} must be {types[0]} [rows][{width}] on {self.device}, not {t.dtype} {list(shape)} on {t.device}")
+        if stride[1] != 1 and width > 1:
+            raise ValueError(f"{name}: the elements of a row must lie together")
+        each = 16 // t.element_size()
+        distance = stride[0] if shape[0] > 1 else (width + each - 1) // each * each
+        if shape[0] > 1 and distance < width:
+            raise ValueError(f"{name}: rows overlap" if writes else f"{name}: rows must lie one behind the other")
+        return t.data_ptr(), shape[0], distance
+
+
+def _type_name(w) -> str:
+    import torch
+    names = {torch.bfloat16: "bf16", torch.float16: "fp16"}
+    if w.dtype not in names:
+        raise ValueError(f"matrices are torch.bfloat16 or torch.float16, not {w.dtype}")
+    return names[w.dtype]
+
+
+class ScaledMatrix(_OnDevice):
+    """A matrix [N][K] held in 8-bit floating point with a power of two for every block of 128 x 128 (duo_scaled_pack), and products of rows with it.
+
+    w: bf16 or fp16 on the GPU, which decides the type of the rows (and the library build); it is not kept.  The calls go to the current stream of
+    the matrix's device and keep no state: calls on several streams, or captured ones, may run side by side."""
+
+    def __init__(self, w):
+        if w.dim() != 2:
+            raise ValueError(f"a matrix has two dimensions, not {w.dim()}")
+        self._settle(w.device, _type_name(w))
+        self.N, self.K = int(w.shape[0]), int(w.shape[1])
+        nbytes = self.lib.duo_scaled_bytes(self.N, self.K)
+        if nbytes == 0:
+            raise ValueError(f"[{self.N}][{self.K}]: K must be a multiple of 32, at most {SCALED_MAX_K}, N at most {SCALED_MAX_N}")
+        w = self._matrix("w", w, self.N, self.K)
+        self._bytes = self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+        self._call("duo_scaled_pack", w.data_ptr(), self.N, self.K, self._bytes.data_ptr())
+        self._ptr = self._bytes.data_ptr()
+        self._in, self._out = (self._element,), (self._element, self._torch.float32)
+
+    @property
+    def packed(self):
+        """The matrix in the layout of duo_scaled_pack (uint8)."""
+        return self._bytes
+
+    def values(self):
+        """fp32 [N][K]: what the stored values stand for."""
+        torch = self._torch
+        nb, kb = (self.N + 127) // 128, (self.K + 127) // 128
+        tiles = nb * kb * 16384
+        q = self._bytes[:tiles].view(torch.float8_e4m3fn).float().reshape(nb, 8, kb, 2, 4, 16, 16)  # row block, band, column block, half, g, row, column
+        scale = torch.ldexp(torch.ones((), device=self.device), self._bytes[tiles:tiles + nb * kb].int() - 127).reshape(nb, 1, kb, 1, 1, 1, 1)
+        return (q * scale).permute(0, 1, 5, 2, 3, 4, 6).reshape(nb * 128, kb * 128)[:self.N, :self.K].contiguous()
+
+    def product(self, x, out=None, fp32: bool = False):
+        """Enqueue y = x' W^T (duo_scaled_gemm), x [rows][K] of the matrix's type brought to e4m3 on the way; returns y: `out` ([rows][N], of that
+        type or fp32), else a new matrix of that type or, with `fp32`, fp32."""
+        torch = self._torch
+        xp, rows, xs = self._rows("x", x, self.K, self._in)
+        if out is None:
+            wide = torch.float32 if fp32 else self._element
+            each = 4 if fp32 else 8
+            out = torch.empty((rows, (self.N + each - 1) // each * each), dtype=wide, device=self.device)[:, :self.N]
+        yp, yrows, ys = self._rows("out", out, self.N, self._out, True)
+        if yrows != rows:
+            raise ValueError(f"out has {yrows} rows, x has {rows}")
+        if rows == 0:
+            return out
+        wp, nbytes = None, 0
+        if rows > DUO_MAX_ROWS:
+            need = C.c_size_t(0)
+            _check(self.lib.duo_scaled_workspace_bytes(rows, self.N, self.K, C.byref(need)), "duo_scaled_workspace_bytes")
+            nbytes = need.value
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)  # of this call and its stream
+            wp = workspace.data_ptr()
+        self._call("duo_scaled_gemm", xp, xs, self._ptr, yp, ys, 1 if out.dtype == torch.float32 else 0, rows, self.N, self.K, wp, nbytes)
+        return out
+
+
+class ExpertLayer(_OnDevice):
+    """A layer of experts for the rows of a verify step (duo_moe_layer): router, choice of top_k experts a row, their SwiGLU MLPs.
+
+    router [n_experts][d_model]; experts: for every expert its gate and up [d_ff][d_model] and down [d_model][d_ff] matrices (any iterable, taken one
+    expert at a time; nothing of it is kept), all bf16 or all fp16 on one GPU.  scaled: the experts are held in the 8-bit blocks of ScaledMatrix.
+    renormalise: a row's shares add up to one.  The calls go to the current stream of the layer's device and keep no state."""
+
+    def __init__(self, router, experts, top_k: int, scaled: bool = False, renormalise: bool = True):
+        if router.dim() != 2:
+            raise ValueError(f"the router is a matrix, not {list(router.shape)}")
+        self._settle(router.device, _type_name(router))
+        torch = self._torch
+        n, d = (int(s) for s in router.shape)
+        self._router = self._matrix("router", router, n, d).clone()
+        self.cfg = self._packed = None
+        taken = 0
+        for e in experts:
+            gate, up, down = e
+            if self.cfg is None:
+                ff = int(gate.shape[0])
+                self.cfg = MoeConfigC(d, ff, n, int(top_k), 1 if scaled else 0, 1 if renormalise else 0)
+                each = self.lib.duo_moe_expert_bytes(C.byref(self.cfg))
+                if each == 0:
+                    raise ValueError(f"{n} experts of d_model {d}, d_ff {ff}, top_k {top_k}: d_model must be a multiple of 64 (at most 8192), d_ff of 32, "
+                                     f"top_k at most the number of experts and {MOE_MAX_TOP}, experts at most {MOE_MAX_EXPERTS}")
+                self._packed = torch.empty(n * each, dtype=torch.uint8, device=self.device)
+            if taken == n:
+                raise ValueError(f"more than {n} experts, the router's rows")
+            m = [self._matrix(name, w, *dims) for name, w, dims in (("gate", gate, (ff, d)), ("up", up, (ff, d)), ("down", down, (d, ff)))]
+            self._call("duo_moe_pack", C.byref(self.cfg), *[w.data_ptr() for w in m], taken, self._packed.data_ptr())
+            taken += 1
+        if taken != n or n == 0:
+            raise ValueError(f"{taken} experts, the router has {n} rows")
+        self.n_experts, self.d_model, self.d_ff, self.top_k = n, d, ff, int(top_k)
+        self.scaled, self.renormalise = bool(scaled), bool(renormalise)
+        self._ref, self._router_ptr, self._experts_ptr = C.byref(self.cfg), self._router.data_ptr(), self._packed.data_ptr()
+        self._types = (self._element,)
+        self._need = {}  # rows -> bytes of workspace
+
+    def _workspace_bytes(self, rows: int) -> int:
+        if rows not in self._need:
+            out = C.c_size_t(0)
+            _check(self.lib.duo_moe_workspace_bytes(self._ref, rows, C.byref(out)), "duo_moe_workspace_bytes")
+            self._need[rows] = out.value
+        return self._need[rows]
+
+    def run(self, x, out=None, position=None, chosen=None, share=None):
+        """Enqueue the layer on x [rows][d_model], at most DUO_MAX_ROWS rows; returns (out, chosen, share): the rows' outputs (`out` may be x), int32
+        [rows][top_k] their experts by descending logit, fp32 [rows][top_k] the shares.  position: int32 [rows] (PagedCache.position of a step), rows
+        with a negative one are left out: their outputs stay as they are (zeros, where this call makes them)."""
+        torch = self._torch
+        xp, rows, xs = self._rows("x", x, self.d_model, self._types)
+        fresh = torch.empty if position is None else torch.zeros
+        if out is None:
+            out = fresh((rows, self.d_model), dtype=self._element, device=self.device)
+        yp, yrows, ys = self._rows("out", out, self.d_model, self._types, True)
+        if yrows != rows:
+            raise ValueError(f"out has {yrows} rows, x has {rows}")
+        given = []
+        for name, t, kind in (("chosen", chosen, torch.int32), ("share", share, torch.float32)):
+            if t is None:
+                t = fresh((rows, self.top_k), dtype=kind, device=self.device)
+            elif t.dtype != kind or tuple(t.shape) != (rows, self.top_k) or t.get_device() != self._index or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {kind} [{rows}][{self.top_k}] on {self.device}, not {t.dtype} {list(t.shape)} on {t.device}")
+            given.append(t)
+        chosen, share = given
+        if position is not None and (position.dtype != torch.int32 or position.dim() != 1 or position.shape[0] < rows or position.get_device() != self._index
+                                     or not position.is_contiguous()):
+            raise ValueError(f"position must be contiguous int32 [{rows}] on {self.device}, not {position.dtype} {list(position.shape)} on {position.device}")
+        if rows == 0:
+            return out, chosen, share
+        need = self._workspace_bytes(rows)
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.device)  # of this call and its stream
+        self._call("duo_moe_layer", self._ref, self._router_ptr, self._experts_ptr, xp, xs, rows, _ptr(position), yp, ys, chosen.data_ptr(),
+                   share.data_ptr(), workspace.data_ptr(), need)
+        return out, chosen, share
 
 
 def spec_sample(logits, root_logits, draft_tokens, draft_probs, uniforms, temperature: float = 1.0,

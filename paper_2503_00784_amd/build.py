@@ -17,7 +17,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 # every source is a code object of its own; the list places the kernels of the first, the step's
-SOURCES = {"duo_api.hip": ["-Xoffload-linker", "--symbol-ordering-file=" + KERNEL_ORDER], "duo_page.hip": []}
+SOURCES = {"duo_api.hip": ["-Xoffload-linker", "--symbol-ordering-file=" + KERNEL_ORDER], "duo_page.hip": [], "duo_scaled.hip": [], "duo_moe.hip": []}
 TYPES = {LIB_PATH: [], LIB_PATH_FP16: ["-DDUO_FP16"]}
 
 

@@ -1,0 +1,125 @@
+// C ABI of the layer of experts: host-side validation and launches (kernels in duo_moe.h).
+#include "../../include/duo_verify.h"
+
+#include "duo_internal.h"
+#include "duo_moe.h"
+
+namespace {
+
+bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool off4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+int check_moe(const duo_moe_config* c) {
+    if (!c) return DUO_ERR_NULL;
+    static_assert(MOE_MAX_EXPERTS == DUO_MOE_MAX_EXPERTS && MOE_MAX_TOP == DUO_MOE_MAX_TOP && MOE_MAX_ROWS == DUO_MAX_ROWS, "what the kernels are laid out for");
+    if (c->d_model < 64 || c->d_model % 64 || c->d_model > 8192 || c->d_ff < 32 || c->d_ff % 32 || c->d_ff > DUO_SCALED_MAX_K) return DUO_ERR_SHAPE;
+    if (c->n_experts < 1 || c->n_experts > DUO_MOE_MAX_EXPERTS || c->top_k < 1 || c->top_k > DUO_MOE_MAX_TOP || c->top_k > c->n_experts) return DUO_ERR_SHAPE;
+    if ((c->scaled != 0 && c->scaled != 1) || (c->renormalise != 0 && c->renormalise != 1)) return DUO_ERR_ARG;
+    return DUO_OK;
+}
+
+size_t matrix_bytes(const duo_moe_config* c, int N, int K) { return c->scaled ? Narrow::bytes(N, K) : Wide::bytes(N, K); }
+size_t expert_bytes(const duo_moe_config* c) { return 2 * matrix_bytes(c, c->d_ff, c->d_model) + matrix_bytes(c, c->d_model, c->d_ff); }
+
+struct MoeLayout {  // of the workspace
+    size_t chosen, share, lists, logits, hidden, total;
+    int ff_pad;
+};
+MoeLayout layout_of(const duo_moe_config* c, int rows) {
+    MoeLayout l{};
+    size_t at = 0;
+    const size_t entries = (size_t)rows * c->top_k;
+    l.ff_pad = c->d_ff;
+    l.chosen = at, at += up16(4 * entries);
+    l.share = at, at += up16(4 * entries);
+    l.lists = at, at += up16(4 * MoeLists::words(moe_most(c->n_experts, rows, c->top_k)));
+    l.logits = at, at += up16(8 * (size_t)rows * c->n_experts);
+    l.hidden = at, at += up16(4 * entries * l.ff_pad);
+    l.total = at;
+    return l;
+}
+
+template <class W, int MT>
+void launch_products(const MoeArgs& a, int most, hipStream_t s) {
+    constexpr int NW = MT > 2 ? 4 : 8;
+    duo_internal_prof(DUO_PROF_MOE_GATEUP);
+    DUO_LAUNCH((moe_gate_up_kernel<W, MT, NW>), dim3(a.ff / 16, most), dim3(64 * NW), s, a);
+    duo_internal_prof(DUO_PROF_MOE_DOWN);
+    DUO_LAUNCH((moe_down_kernel<W, MT, 8>), dim3(a.d / 16), dim3(512), s, a);
+}
+template <class W>
+void launch_products(const MoeArgs& a, int most, hipStream_t s) {
+    switch ((a.rows + 15) / 16) {
+        case 1: return launch_products<W, 1>(a, most, s);
+        case 2: return launch_products<W, 2>(a, most, s);
+        case 3: return launch_products<W, 3>(a, most, s);
+        case 4: return launch_products<W, 4>(a, most, s);
+        default: return launch_products<W, 5>(a, most, s);
+    }
+}
+
+}  // namespace
+
+extern "C" size_t duo_moe_expert_bytes(const duo_moe_config* cfg) { return check_moe(cfg) ? 0 : expert_bytes(cfg); }
+
+extern "C" int duo_moe_pack(const duo_moe_config* cfg, const uint16_t* w_gate, const uint16_t* w_up, const uint16_t* w_down, int expert, void* experts,
+                            void* hip_stream) {
+    if (const int rc = check_moe(cfg)) return rc;
+    if (!w_gate || !w_up || !w_down || !experts) return DUO_ERR_NULL;
+    if (expert < 0 || expert >= cfg->n_experts) return DUO_ERR_ARG;
+    if (off16(w_gate) || off16(w_up) || off16(w_down) || off16(experts)) return DUO_ERR_ALIGN;
+    const int d = cfg->d_model, ff = cfg->d_ff;
+    const uint16_t* const src[3] = {w_gate, w_up, w_down};
+    char* dst = static_cast<char*>(experts) + (size_t)expert * expert_bytes(cfg);
+    for (int i = 0; i < 3; ++i) {
+        const int N = i < 2 ? ff : d, K = i < 2 ? d : ff;
+        const int rc = cfg->scaled ? duo_scaled_pack(src[i], N, K, dst, hip_stream) : duo_pack_matrix(src[i], N, K, reinterpret_cast<uint16_t*>(dst), hip_stream);
+        if (rc) return rc;
+        dst += matrix_bytes(cfg, N, K);
+    }
+    return DUO_OK;
+}
+
+extern "C" int duo_moe_workspace_bytes(const duo_moe_config* cfg, int rows, size_t* bytes) {
+    if (!bytes) return DUO_ERR_NULL;
+    if (const int rc = check_moe(cfg)) return rc;
+    if (rows < 1 || rows > DUO_MAX_ROWS) return DUO_ERR_SHAPE;
+    *bytes = layout_of(cfg, rows).total;
+    return DUO_OK;
+}
+
+extern "C" int duo_moe_layer(const duo_moe_config* cfg, const uint16_t* router, const void* experts, const uint16_t* x, int64_t x_stride, int rows,
+                             const int32_t* position, uint16_t* y, int64_t y_stride, int32_t* chosen, float* share, void* workspace,
+                             size_t workspace_bytes, void* hip_stream) {
+    if (const int rc = check_moe(cfg)) return rc;
+    if (!router || !experts || !x || !y || !workspace) return DUO_ERR_NULL;
+    if (rows < 1 || rows > DUO_MAX_ROWS) return DUO_ERR_SHAPE;
+    if (off16(router) || off16(experts) || off16(x) || off16(y) || off16(workspace) || x_stride % 8 || y_stride % 8) return DUO_ERR_ALIGN;
+    if (off4(position) || off4(chosen) || off4(share)) return DUO_ERR_ALIGN;
+    const int d = cfg->d_model;
+    if (rows > 1 && (x_stride < d || y_stride < d || x_stride > DUO_SCALED_MAX_STRIDE || y_stride > DUO_SCALED_MAX_STRIDE)) return DUO_ERR_SHAPE;
+    const MoeLayout lay = layout_of(cfg, rows);
+    if (workspace_bytes < lay.total) return DUO_ERR_WORKSPACE;
+    char* const ws = static_cast<char*>(workspace);
+    MoeArgs a{};
+    a.x = x, a.y = y, a.router = router, a.experts = static_cast<const uint8_t*>(experts), a.position = position;
+    a.chosen = chosen ? chosen : reinterpret_cast<int32_t*>(ws + lay.chosen);
+    a.share = share ? share : reinterpret_cast<float*>(ws + lay.share);
+    a.lists = reinterpret_cast<int32_t*>(ws + lay.lists);
+    a.logits = reinterpret_cast<double*>(ws + lay.logits);
+    a.hidden = reinterpret_cast<u16*>(ws + lay.hidden);
+    a.x_stride = x_stride, a.y_stride = y_stride;
+    a.expert_bytes = expert_bytes(cfg), a.up_at = matrix_bytes(cfg, cfg->d_ff, d), a.down_at = 2 * a.up_at;
+    a.rows = rows, a.d = d, a.ff = cfg->d_ff, a.ff_pad = lay.ff_pad, a.n_experts = cfg->n_experts, a.top = cfg->top_k, a.renormalise = cfg->renormalise;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    duo_internal_prof(DUO_PROF_MOE_ROUTER);
+    DUO_LAUNCH(moe_logits_kernel, dim3((a.n_experts + 3) / 4, rows), dim3(256), s, a);
+    duo_internal_prof(DUO_PROF_MOE_ROUTER);
+    DUO_LAUNCH(moe_select_kernel, dim3(1), dim3(1024), s, a);
+    const int most = moe_most(a.n_experts, rows, a.top);
+    if (cfg->scaled) launch_products<Narrow>(a, most, s);
+    else launch_products<Wide>(a, most, s);
+    return duo_internal_hip_ok(hipGetLastError(), "duo_moe_layer");
+}

@@ -1,0 +1,92 @@
+// C ABI of the products on 8-bit matrices: host-side validation and launches (kernels in duo_scaled.h).
+#include "../../include/duo_verify.h"
+
+#include "duo_internal.h"
+#include "duo_scaled.h"
+
+namespace {
+
+bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+int check_matrix(int N, int K) { return N < 1 || N > DUO_SCALED_MAX_N || K < 32 || K % 32 || K > DUO_SCALED_MAX_K ? DUO_ERR_SHAPE : DUO_OK; }
+
+size_t rows_bytes(int rows, int K) {  // of the workspace: tiles and scales of the activations
+    const size_t tiles = (size_t)(rows + 15) / 16, blocks = scaled_blocks(K);
+    return rows <= DUO_MAX_ROWS ? 0 : tiles * blocks * (SCALED_TILE + 16);
+}
+
+template <int MT, bool FP32>
+void launch_stream(const ScaledArgs& a, hipStream_t s) {
+    constexpr int NB = 1, NW = MT > 3 ? 4 : 8;
+    const int bands = (a.N + 15) / 16;
+    duo_internal_prof(DUO_PROF_SCALED);
+    DUO_LAUNCH((scaled_stream_kernel<MT, NB, NW, FP32>), dim3((bands + NB - 1) / NB), dim3(64 * NW), s, a);
+}
+
+template <bool FP32>
+void launch_product(const ScaledArgs& a, hipStream_t s) {
+    switch (a.rows <= DUO_MAX_ROWS ? a.row_tiles : 0) {
+        case 1: return launch_stream<1, FP32>(a, s);
+        case 2: return launch_stream<2, FP32>(a, s);
+        case 3: return launch_stream<3, FP32>(a, s);
+        case 4: return launch_stream<4, FP32>(a, s);
+        case 5: return launch_stream<5, FP32>(a, s);
+    }
+    duo_internal_prof(DUO_PROF_SCALED);
+    DUO_LAUNCH(scaled_rows_kernel, dim3(a.KB, (a.row_tiles + 3) / 4), dim3(256), s, a);
+    duo_internal_prof(DUO_PROF_SCALED);
+    DUO_LAUNCH((scaled_block_kernel<FP32>), dim3(scaled_blocks(a.N), (a.row_tiles + 7) / 8), dim3(256), s, a);
+}
+
+}  // namespace
+
+extern "C" size_t duo_scaled_bytes(int N, int K) { return check_matrix(N, K) ? 0 : scaled_bytes(N, K); }
+
+extern "C" int duo_scaled_pack(const uint16_t* src, int N, int K, void* dst, void* hip_stream) {
+    if (!src || !dst) return DUO_ERR_NULL;
+    if (const int rc = check_matrix(N, K)) return rc;
+    if (off16(src) || off16(dst)) return DUO_ERR_ALIGN;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    DUO_LAUNCH(scaled_pack_kernel, dim3(scaled_blocks(K), scaled_blocks(N)), dim3(256), s, src, N, K, static_cast<uint8_t*>(dst));
+    return duo_internal_hip_ok(hipGetLastError(), "duo_scaled_pack");
+}
+
+extern "C" int duo_scaled_workspace_bytes(int rows, int N, int K, size_t* bytes) {
+    if (!bytes) return DUO_ERR_NULL;
+    if (const int rc = check_matrix(N, K)) return rc;
+    if (rows < 1 || rows > DUO_SCALED_MAX_ROWS) return DUO_ERR_SHAPE;
+    *bytes = rows_bytes(rows, K);
+    return DUO_OK;
+}
+
+extern "C" int duo_scaled_gemm(const uint16_t* x, int64_t x_stride, const void* w, void* y, int64_t y_stride, int y_fp32, int rows, int N, int K,
+                               void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!x || !w || !y) return DUO_ERR_NULL;
+    if (const int rc = check_matrix(N, K)) return rc;
+    if (rows < 1 || rows > DUO_SCALED_MAX_ROWS) return DUO_ERR_SHAPE;
+    if (y_fp32 != 0 && y_fp32 != 1) return DUO_ERR_ARG;
+    if (off16(x) || off16(w) || off16(y) || x_stride % 8 || y_stride % (y_fp32 ? 4 : 8)) return DUO_ERR_ALIGN;
+    if (rows > 1 && (x_stride < K || y_stride < N || x_stride > DUO_SCALED_MAX_STRIDE || y_stride > DUO_SCALED_MAX_STRIDE)) return DUO_ERR_SHAPE;
+    // what is written meets nothing that other workgroups still read
+    const char *x0 = reinterpret_cast<const char*>(x), *y0 = static_cast<const char*>(y), *w0 = static_cast<const char*>(w);
+    const int64_t last = rows - 1;
+    const char *x1 = x0 + 2 * (last * x_stride + K), *y1 = y0 + (y_fp32 ? 4 : 2) * (last * y_stride + N), *w1 = w0 + scaled_bytes(N, K);
+    if ((y0 < x1 && x0 < y1) || (y0 < w1 && w0 < y1)) return DUO_ERR_ARG;
+    const size_t need = rows_bytes(rows, K);
+    if (need) {
+        if (!workspace) return DUO_ERR_NULL;
+        if (off16(workspace)) return DUO_ERR_ALIGN;
+        if (workspace_bytes < need) return DUO_ERR_WORKSPACE;
+    }
+    ScaledArgs a{};
+    a.x = x, a.w = static_cast<const uint8_t*>(w), a.y = y, a.xq = static_cast<uint8_t*>(workspace);
+    a.x_stride = x_stride, a.y_stride = y_stride;
+    a.rows = rows, a.N = N, a.K = K, a.KB = scaled_blocks(K), a.row_tiles = (rows + 15) / 16;
+    a.w_scales = scaled_tile_bytes(N, K), a.x_scales = (size_t)a.row_tiles * a.KB * SCALED_TILE;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // not of an earlier call
+    if (y_fp32) launch_product<true>(a, s);
+    else launch_product<false>(a, s);
+    return duo_internal_hip_ok(hipGetLastError(), "duo_scaled_gemm");
+}
