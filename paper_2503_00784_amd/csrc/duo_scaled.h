@@ -1,20 +1,48 @@
 // Products on matrices in e4m3 with block scales: packing, a kernel that streams the matrix past a few rows, and one for many rows.
 #pragma once
+#include <type_traits>
+
 #include "duo_e4m3.h"
+
+struct ScaledArgs {
+    const u16* x;          // [rows][K], x_stride elements from row to row
+    const uint8_t* w;      // tiles, then the scales
+    void* y;               // 16-bit or fp32 [rows][N]
+    uint8_t* xq;           // rows brought to e4m3 beforehand: their tiles, then their scales (see row_scale_at)
+    size_t w_scales, x_scales;  // bytes in front of the scales
+    int64_t x_stride, y_stride;
+    int rows, N, K, KB, row_tiles;
+};
+
+// Scales of rows: byte + 127 of (block j, row tile, row c of it), so that one word holds a row's place in four tiles, as the matrix instruction picks them.
+__host__ __device__ inline size_t row_scale_bytes(int row_tiles, int KB) { return (size_t)KB * ((row_tiles + 3) / 4) * 64; }
+__device__ __forceinline__ size_t row_scale_at(int row_tiles, int j, int tile, int c) {
+    return (((size_t)j * ((row_tiles + 3) >> 2) + (tile >> 2)) * 16 + c) * 4 + (tile & 3);
+}
 
 // 32 values of a row as a lane of an operand holds them: columns 64 h + 16 g + 8 i .. +8 of a block in v[2 h + i], g = lane / 16.
 struct RowPiece {
     u32x4 v[4];
-    // row: the row's first element, or null for a row of zeros; k: first column of the block; columns from K on are zeros (K % 32 == 0)
+    // row: the row's first element; k: first column of the block.  Columns from K on (K % 32 == 0) are not read: what stands for them is, until
+    // `cut` is called.
     __device__ __forceinline__ void load(const u16* row, int k, int K, int g) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int c = k + 64 * h + 16 * g;
-            const bool in = row != nullptr && c < K;
-            const u32x4* p = reinterpret_cast<const u32x4*>(row + c);
-            v[2 * h] = in ? p[0] : u32x4{0u, 0u, 0u, 0u};
-            v[2 * h + 1] = in ? p[1] : u32x4{0u, 0u, 0u, 0u};
+            const u32x4* p = reinterpret_cast<const u32x4*>(row + (c < K ? c : 0));
+            v[2 * h] = p[0];
+            v[2 * h + 1] = p[1];
         }
+    }
+    // zeros in the columns from K on
+    __device__ __forceinline__ void cut(int k, int K, int g) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (k + 64 * h + 16 * g >= K) v[2 * h] = v[2 * h + 1] = u32x4{0u, 0u, 0u, 0u};
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
     }
     // e + 127 of the block this row has here: the largest magnitude of the four lanes that share the row.  Infinities and NaN count too: their row
     // is NaN whatever becomes of its other values.
@@ -31,6 +59,18 @@ struct RowPiece {
         m = max(b[0], b[1]);
         return scale_byte(m);
     }
+    using Source = const u16*;
+    static __device__ __forceinline__ Source source(const ScaledArgs& a, int tile, int lane) {
+        return a.x + (int64_t)min(tile * 16 + (lane & 15), a.rows - 1) * a.x_stride;
+    }
+    __device__ __forceinline__ void load(Source row, int j, const ScaledArgs& a, int g) { load(row, j * SCALE_BLOCK, a.K, g); }
+    // the block in e4m3, returns its scale
+    __device__ __forceinline__ float e4m3(int k, int K, int g, u32x4 (&q)[2]) {
+        if (k + SCALE_BLOCK > K) cut(k, K, g);
+        const float s = scale_of(scale());
+        quantise(s, q);
+        return s;
+    }
     __device__ __forceinline__ void quantise(float s, u32x4 (&q)[2]) const {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -39,6 +79,28 @@ struct RowPiece {
                 q[h][2 * i] = to_e4m3(v[2 * h + i][0], v[2 * h + i][1], s);
                 q[h][2 * i + 1] = to_e4m3(v[2 * h + i][2], v[2 * h + i][3], s);
             }
+    }
+};
+
+// the same from rows that scaled_rows_kernel has brought to e4m3
+struct ReadyPiece {
+    u32x4 v[2];
+    int byte;
+    struct Source {
+        const u32x4* tile;
+        const uint8_t* scale;
+    };
+    static __device__ __forceinline__ Source source(const ScaledArgs& a, int tile, int lane) {
+        return {reinterpret_cast<const u32x4*>(a.xq + (size_t)tile * a.KB * SCALED_TILE) + lane, a.xq + a.x_scales + row_scale_at(a.row_tiles, 0, tile, lane & 15)};
+    }
+    __device__ __forceinline__ void load(Source s, int j, const ScaledArgs& a, int) {
+        v[0] = s.tile[(size_t)j * (SCALED_TILE / 16)];
+        v[1] = s.tile[(size_t)j * (SCALED_TILE / 16) + 64];
+        byte = s.scale[row_scale_at(a.row_tiles, j, 0, 0)];
+    }
+    __device__ __forceinline__ float e4m3(int, int, int, u32x4 (&q)[2]) {
+        q[0] = v[0], q[1] = v[1];
+        return scale_of(byte);
     }
 };
 
@@ -53,7 +115,9 @@ __global__ __launch_bounds__(256) void scaled_pack_kernel(const u16* __restrict_
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int row = rb * SCALE_BLOCK + (2 * wave + i) * 16 + r;
-        x[i].load(row < N ? src + (size_t)row * K : nullptr, j * SCALE_BLOCK, K, g);
+        x[i].load(src + (size_t)min(row, N - 1) * K, j * SCALE_BLOCK, K, g);
+        x[i].cut(j * SCALE_BLOCK, K, g);
+        if (row >= N) x[i].clear();
 #pragma unroll
         for (int a = 0; a < 4; ++a)
 #pragma unroll
@@ -80,16 +144,6 @@ __global__ __launch_bounds__(256) void scaled_pack_kernel(const u16* __restrict_
     if (threadIdx.x == 0) dst[scaled_tile_bytes(N, K) + (size_t)rb * KB + j] = (uint8_t)byte;
 }
 
-struct ScaledArgs {
-    const u16* x;          // [rows][K], x_stride elements from row to row
-    const uint8_t* w;      // tiles, then the scales
-    void* y;               // 16-bit or fp32 [rows][N]
-    uint8_t* xq;           // many rows: tiles of the activations, then their scales [K / 128][row tiles * 16]
-    size_t w_scales, x_scales;  // bytes in front of the scales
-    int64_t x_stride, y_stride;
-    int rows, N, K, KB, row_tiles;
-};
-
 // four consecutive outputs (features n .. n + 3) of one row; n and the strides are multiples of 4, so the store is as wide as it looks
 template <bool FP32>
 __device__ __forceinline__ void store_outputs(const ScaledArgs& a, int row, int n, f32x4 v) {
@@ -109,47 +163,77 @@ __device__ __forceinline__ void store_outputs(const ScaledArgs& a, int row, int 
 }
 
 // ---- few rows: a workgroup owns NB bands, its NW waves take the blocks of columns in turn and add up what they have through LDS, in wave order.
-template <int MT, int NB, int NW, bool FP32>
+// PF blocks of a wave are on their way at any time; the loads are the same ones whatever the sizes (clamped, not skipped), so that the compiler can
+// count them instead of waiting for all.  Rows behind the last are the last one again: they are columns of the product that nobody stores.
+// Where READY, the rows lie in `xq` as scaled_rows_kernel leaves them.
+template <int MT, int NB, int NW, int PF, bool READY, bool FP32>
 __global__ __launch_bounds__(64 * NW) void scaled_stream_kernel(ScaledArgs a) {
     __shared__ f32x4 part[NW][NB * MT][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int band0 = blockIdx.x * NB, last = scaled_blocks(a.N) * 8 - 1;
-    const u16* row[MT];
+    const int band0 = blockIdx.x * NB;  // a multiple of NB, which divides 8: the bands share a block of rows, and its scale
+    using Rows = typename std::conditional<READY, ReadyPiece, RowPiece>::type;
+    typename Rows::Source row[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) row[m] = m * 16 + c < a.rows ? a.x + (int64_t)(m * 16 + c) * a.x_stride : nullptr;
+    for (int m = 0; m < MT; ++m) row[m] = Rows::source(a, m, lane);
+    const u32x4* tiles = reinterpret_cast<const u32x4*>(a.w + (size_t)band0 * a.KB * SCALED_TILE) + lane;
+    const uint8_t* scales = a.w + a.w_scales + (size_t)(band0 >> 3) * a.KB;
     f32x4 acc[NB][MT];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[b][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int j = wave; j < a.KB; j += NW) {
+
+    u32x4 wq[PF][NB][2];
+    int sw[PF];
+    Rows xs[PF][MT];
+    const int n = (a.KB - wave + NW - 1) / NW;  // blocks of this wave: wave, wave + NW, ...
+    auto block = [&](int i) { return min(wave + NW * min(i, n - 1), a.KB - 1); };
+    auto load = [&](int s, int i) {
+        const int j = max(block(i), 0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wq[s][b][h] = __builtin_nontemporal_load(tiles + ((size_t)b * a.KB + j) * (SCALED_TILE / 16) + 64 * h);
+        sw[s] = scales[j];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xs[s][m].load(row[m], j, a, g);
+    };
+    auto products = [&](int s, int i) {
+        const int j = wave + NW * i;
+        const float scale = scale_of(sw[s]);
         bf16x8 w[NB][4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int band = min(band0 + b, last);
-            const u32x4* tile = reinterpret_cast<const u32x4*>(a.w + ((size_t)band * a.KB + j) * SCALED_TILE) + lane;
-            const u32x4 q0 = __builtin_nontemporal_load(tile), q1 = __builtin_nontemporal_load(tile + 64);
-            const float s = scale_of(a.w[a.w_scales + (size_t)(band >> 3) * a.KB + j]);
-            w[b][0] = e4m3_to_bf16(q0[0], q0[1], s);
-            w[b][1] = e4m3_to_bf16(q0[2], q0[3], s);
-            w[b][2] = e4m3_to_bf16(q1[0], q1[1], s);
-            w[b][3] = e4m3_to_bf16(q1[2], q1[3], s);
-        }
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[b][q] = e4m3_to_bf16(wq[s][b][q >> 1][2 * (q & 1)], wq[s][b][q >> 1][2 * (q & 1) + 1], scale);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            RowPiece x;
+            Rows x = xs[s][m];
             u32x4 q[2];
-            x.load(row[m], j * SCALE_BLOCK, a.K, g);
-            const float s = scale_of(x.scale());
-            x.quantise(s, q);
+            const float sx = x.e4m3(j * SCALE_BLOCK, a.K, g, q);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x8 v = e4m3_to_bf16(q[i >> 1][2 * (i & 1)], q[i >> 1][2 * (i & 1) + 1], s);
+            for (int k = 0; k < 4; ++k) {
+                const bf16x8 v = e4m3_to_bf16(q[k >> 1][2 * (k & 1)], q[k >> 1][2 * (k & 1) + 1], sx);
 #pragma unroll
-                for (int b = 0; b < NB; ++b) acc[b][m] = mfma_bf16(w[b][i], v, acc[b][m]);
+                for (int b = 0; b < NB; ++b) acc[b][m] = mfma_bf16(w[b][k], v, acc[b][m]);
             }
         }
+    };
+#pragma unroll
+    for (int s = 0; s < PF; ++s) load(s, s);
+    int i = 0;
+    for (; i + PF < n; i += PF) {
+#pragma unroll
+        for (int s = 0; s < PF; ++s) {
+            products(s, i + s);
+            load(s, i + s + PF);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
+#pragma unroll
+    for (int s = 0; s < PF; ++s)
+        if (i + s < n) products(s, i + s);
+
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -170,65 +254,119 @@ __global__ __launch_bounds__(256) void scaled_rows_kernel(ScaledArgs a) {
     const int r = tile * 16 + c;
     RowPiece x;
     u32x4 q[2];
-    x.load(r < a.rows ? a.x + (int64_t)r * a.x_stride : nullptr, j * SCALE_BLOCK, a.K, g);
+    x.load(a.x + (int64_t)min(r, a.rows - 1) * a.x_stride, j * SCALE_BLOCK, a.K, g);
+    x.cut(j * SCALE_BLOCK, a.K, g);
     const int byte = x.scale();
     x.quantise(scale_of(byte), q);
     u32x4* dst = reinterpret_cast<u32x4*>(a.xq + ((size_t)tile * a.KB + j) * SCALED_TILE);
     dst[lane] = q[0];
     dst[64 + lane] = q[1];
-    if (g == 0) a.xq[a.x_scales + ((size_t)j * a.row_tiles + tile) * 16 + c] = (uint8_t)byte;
+    if (g == 0) a.xq[a.x_scales + row_scale_at(a.row_tiles, j, tile, c)] = (uint8_t)byte;
 }
 
-// then the product: four waves, each 4 bands x 4 row tiles.
-template <bool FP32>
-__global__ __launch_bounds__(256) void scaled_block_kernel(ScaledArgs a) {
+// then the product.  GB x GM waves, each WB bands x WM row tiles, on a block of features x rows.  Both operands lie in tiles as the matrix units take
+// them, so a stage (128 columns of the block) is a list of 1 KiB pieces that go from global memory straight into LDS, one lane's 16 bytes behind the
+// other's, and are read back the same way: no bank conflicts, no registers on the way.  Two stages: the next one is requested right behind the
+// barrier that says that everybody has left its place, and has all the products of this one to arrive.
+// 16-bit outputs use the 8-bit instruction, which applies the scales itself (a byte of a word for every row and block); fp32 outputs use the
+// 16-bit instruction on values that were converted with their scales, exactly, at half the rate.
+template <int WB, int WM, int GB, int GM, bool FP32>
+__global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a) {
+    constexpr int WAVES = GB * GM, BB = WB * GB, BM = WM * GM;  // bands and row tiles of the block
+    constexpr int PIECES = 2 * (BB + BM), EACH = PIECES / WAVES;
+    static_assert(PIECES % WAVES == 0 && WM == 4 && 8 % WB == 0, "equal loads for all; a wave's row tiles share a word of scales, its bands a scale");
+    __shared__ u32x4 lds[2][PIECES * 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int band0 = blockIdx.x * 8 + (wave & 1) * 4, tile0 = blockIdx.y * 8 + (wave >> 1) * 4;
-    f32x4 acc[4][4];
+    // Workgroups are dealt to the eight dies in turn.  Each die gets a run of neighbouring blocks: four blocks of rows by as many of features, so
+    // that what a die reads at a time is shared by many of its workgroups.
+    const int feature_blocks = (scaled_blocks(a.N) * 8 + BB - 1) / BB, row_blocks = (a.row_tiles + BM - 1) / BM, blocks = feature_blocks * row_blocks;
+    const int share = (blocks + 7) / 8, id = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= share || id >= blocks) return;
+    const int band_of_four = id / (4 * feature_blocks), in_four = id - band_of_four * 4 * feature_blocks;
+    const int tall = min(4, row_blocks - band_of_four * 4);
+    const int rb = band_of_four * 4 + in_four % tall, fb = in_four / tall;
+    const int band_last = scaled_blocks(a.N) * 8 - 1, tile_last = a.row_tiles - 1;
+    const int wb = wave % GB, wm = wave / GB;
+    const int band0 = fb * BB + wb * WB, tile0 = rb * BM + wm * WM;
+
+    const u32x4* from[EACH];  // pieces wave * EACH .. of a stage: half (piece & 1) of a band's or a row tile's tile; beyond the ends the last one again
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int i = 0; i < EACH; ++i) {
+        const int piece = wave * EACH + i, t = piece >> 1;
+        const uint8_t* p = t < BB ? a.w + (size_t)min(fb * BB + t, band_last) * a.KB * SCALED_TILE : a.xq + (size_t)min(rb * BM + t - BB, tile_last) * a.KB * SCALED_TILE;
+        from[i] = reinterpret_cast<const u32x4*>(p + (piece & 1) * 1024) + lane;
+    }
+    const uint8_t* w_scale = a.w + a.w_scales + (size_t)(min(band0, band_last) >> 3) * a.KB;
+    const uint8_t* x_scale = a.xq + a.x_scales + row_scale_at(a.row_tiles, 0, min(tile0, tile_last) & ~3, c);
+    const size_t x_step = row_scale_at(a.row_tiles, 1, 0, 0);
+    auto request = [&](int j) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) acc[b][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < EACH; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[i] + (size_t)j * (SCALED_TILE / 16)),
+                                             (__attribute__((address_space(3))) void*)(&lds[j & 1][(wave * EACH + i) * 64]), 16, 0, 0);
+    };
+    f32x4 acc[WB][WM];
+#pragma unroll
+    for (int b = 0; b < WB; ++b)
+#pragma unroll
+        for (int m = 0; m < WM; ++m) acc[b][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    request(0);
+    int sw_next = w_scale[0], sx_next = *reinterpret_cast<const int*>(x_scale);
     for (int j = 0; j < a.KB; ++j) {
-        u32x4 w[4][2], x[4][2];
-        int sx[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x4* wt = reinterpret_cast<const u32x4*>(a.w + ((size_t)(band0 + i) * a.KB + j) * SCALED_TILE) + lane;
-            w[i][0] = wt[0], w[i][1] = wt[64];
-            const int tile = min(tile0 + i, a.row_tiles - 1);
-            const u32x4* xt = reinterpret_cast<const u32x4*>(a.xq + ((size_t)tile * a.KB + j) * SCALED_TILE) + lane;
-            x[i][0] = xt[0], x[i][1] = xt[64];
-            sx[i] = a.xq[a.x_scales + ((size_t)j * a.row_tiles + tile) * 16 + c];
+        const int sw = sw_next, sx = sx_next;
+        __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): this wave's pieces of stage j have landed
+        __builtin_amdgcn_s_barrier();                      // and everybody's; nobody reads stage j - 1 any more
+        if (j + 1 < a.KB) {
+            request(j + 1);
+            sw_next = w_scale[j + 1];
+            sx_next = *reinterpret_cast<const int*>(x_scale + (size_t)(j + 1) * x_step);
         }
-        const int sw = a.w[a.w_scales + (size_t)(band0 >> 3) * a.KB + j];
+        const u32x4* stage = &lds[j & 1][lane];
+        const u32x4 *ws = stage + wb * WB * 128, *xs = stage + (BB + wm * WM) * 128;
         if constexpr (FP32) {
+            const float fw = scale_of(sw);
+            float fx[4];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                bf16x8 v[4], u[4];
+            for (int m = 0; m < 4; ++m) fx[m] = scale_of(sx >> (8 * m) & 255);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] = e4m3_to_bf16(w[i][s >> 1][2 * (s & 1)], w[i][s >> 1][2 * (s & 1) + 1], scale_of(sw));
-                    u[i] = e4m3_to_bf16(x[i][s >> 1][2 * (s & 1)], x[i][s >> 1][2 * (s & 1) + 1], scale_of(sx[i]));
+            for (int h = 0; h < 2; ++h) {
+                u32x4 x[WM];
+#pragma unroll
+                for (int m = 0; m < WM; ++m) x[m] = xs[m * 128 + h * 64];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    bf16x8 u[WM];
+#pragma unroll
+                    for (int m = 0; m < WM; ++m) u[m] = e4m3_to_bf16(x[m][2 * i], x[m][2 * i + 1], fx[m]);
+#pragma unroll
+                    for (int b = 0; b < WB; ++b) {
+                        const u32x4 w = ws[b * 128 + h * 64];
+                        const bf16x8 v = e4m3_to_bf16(w[2 * i], w[2 * i + 1], fw);
+#pragma unroll
+                        for (int m = 0; m < WM; ++m) acc[b][m] = mfma_bf16(v, u[m], acc[b][m]);
+                    }
                 }
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) acc[b][m] = mfma_bf16(v[b], u[m], acc[b][m]);
             }
         } else {
-            auto both = [](const u32x4 (&q)[2]) {
-                return i32x8{(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[1][0], (int)q[1][1], (int)q[1][2], (int)q[1][3]};
+            auto whole = [](const u32x4* t) {
+                const u32x4 p = t[0], q = t[64];
+                return i32x8{(int)p[0], (int)p[1], (int)p[2], (int)p[3], (int)q[0], (int)q[1], (int)q[2], (int)q[3]};
             };
+            i32x8 x[WM];
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int m = 0; m < WM; ++m) x[m] = whole(xs + m * 128);
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
-                    acc[b][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(w[b]), both(x[m]), acc[b][m], 0, 0, 0, sw, 0, sx[m]);
+            for (int b = 0; b < WB; ++b) {
+                const i32x8 w = whole(ws + b * 128);
+                acc[b][0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[0], acc[b][0], 0, 0, 0, sw, 0, sx);
+                acc[b][1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[1], acc[b][1], 0, 0, 0, sw, 1, sx);
+                acc[b][2] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[2], acc[b][2], 0, 0, 0, sw, 2, sx);
+                acc[b][3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[3], acc[b][3], 0, 0, 0, sw, 3, sx);
+            }
         }
     }
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < WB; ++b)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) store_outputs<FP32>(a, (tile0 + m) * 16 + c, (band0 + b) * 16 + 4 * g, acc[b][m]);
+        for (int m = 0; m < WM; ++m) store_outputs<FP32>(a, (tile0 + m) * 16 + c, (band0 + b) * 16 + 4 * g, acc[b][m]);
 }

@@ -10,21 +10,41 @@ bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; 
 
 int check_matrix(int N, int K) { return N < 1 || N > DUO_SCALED_MAX_N || K < 32 || K % 32 || K > DUO_SCALED_MAX_K ? DUO_ERR_SHAPE : DUO_OK; }
 
-size_t rows_bytes(int rows, int K) {  // of the workspace: tiles and scales of the activations
-    const size_t tiles = (size_t)(rows + 15) / 16, blocks = scaled_blocks(K);
-    return rows <= DUO_MAX_ROWS ? 0 : tiles * blocks * (SCALED_TILE + 16);
+size_t rows_bytes(int rows, int K) {  // of the workspace: tiles and scales of the rows
+    const int tiles = (rows + 15) / 16, blocks = scaled_blocks(K);
+    return rows <= DUO_SCALED_DIRECT_ROWS ? 0 : (size_t)tiles * blocks * SCALED_TILE + row_scale_bytes(tiles, blocks);
 }
 
-template <int MT, bool FP32>
-void launch_stream(const ScaledArgs& a, hipStream_t s) {
-    constexpr int NB = 1, NW = MT > 3 ? 4 : 8;
+template <int MT, int NB, int NW, int PF, bool FP32>
+void launch_bands(const ScaledArgs& a, hipStream_t s) {
     const int bands = (a.N + 15) / 16;
     duo_internal_prof(DUO_PROF_SCALED);
-    DUO_LAUNCH((scaled_stream_kernel<MT, NB, NW, FP32>), dim3((bands + NB - 1) / NB), dim3(64 * NW), s, a);
+    DUO_LAUNCH((scaled_stream_kernel<MT, NB, NW, PF, (MT > DUO_SCALED_DIRECT_ROWS / 16), FP32>), dim3((bands + NB - 1) / NB), dim3(64 * NW), s, a);
+}
+template <int MT, bool FP32>
+void launch_stream(const ScaledArgs& a, hipStream_t s) {
+    const int bands = (a.N + 15) / 16;
+    if (bands <= 256) launch_bands<MT, 1, 8, (MT == 2 ? 1 : 2), FP32>(a, s);
+    else if (bands <= 512) launch_bands<MT, 2, 8, (MT == 2 ? 1 : 2), FP32>(a, s);
+    else if (bands <= 1024) launch_bands<MT, 4, (MT == 2 ? 4 : 8), (MT == 2 ? 2 : 1), FP32>(a, s);
+    else if constexpr (MT == 1) launch_bands<MT, 2, 8, 2, FP32>(a, s);
+    else if constexpr (MT == 2) launch_bands<MT, 4, 4, 1, FP32>(a, s);
+    else launch_bands<MT, 4, 2, 2, FP32>(a, s);
+}
+int blocks_of(const ScaledArgs& a, int bands, int tiles) { return (scaled_blocks(a.N) * 8 + bands - 1) / bands * ((a.row_tiles + tiles - 1) / tiles); }
+template <int WB, int WM, int GB, int GM, bool FP32>
+void launch_block(const ScaledArgs& a, hipStream_t s) {
+    const int blocks = blocks_of(a, WB * GB, WM * GM);
+    duo_internal_prof(DUO_PROF_SCALED);
+    DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, FP32>), dim3((blocks + 7) / 8 * 8), dim3(64 * GB * GM), s, a);
 }
 
 template <bool FP32>
 void launch_product(const ScaledArgs& a, hipStream_t s) {
+    if (a.rows > DUO_SCALED_DIRECT_ROWS) {
+        duo_internal_prof(DUO_PROF_SCALED);
+        DUO_LAUNCH(scaled_rows_kernel, dim3(a.KB, (a.row_tiles + 3) / 4), dim3(256), s, a);
+    }
     switch (a.rows <= DUO_MAX_ROWS ? a.row_tiles : 0) {
         case 1: return launch_stream<1, FP32>(a, s);
         case 2: return launch_stream<2, FP32>(a, s);
@@ -32,10 +52,14 @@ void launch_product(const ScaledArgs& a, hipStream_t s) {
         case 4: return launch_stream<4, FP32>(a, s);
         case 5: return launch_stream<5, FP32>(a, s);
     }
-    duo_internal_prof(DUO_PROF_SCALED);
-    DUO_LAUNCH(scaled_rows_kernel, dim3(a.KB, (a.row_tiles + 3) / 4), dim3(256), s, a);
-    duo_internal_prof(DUO_PROF_SCALED);
-    DUO_LAUNCH((scaled_block_kernel<FP32>), dim3(scaled_blocks(a.N), (a.row_tiles + 7) / 8), dim3(256), s, a);
+    // Blocks of 256 x 256, one to a compute unit, or of 128 x 128, two to one: two of the small ones take 0.54 of the time of a large one (8192^3: 452
+    // us against 484), so what decides is how the last round comes out (999 rows, 5120 x 13824: 159 us in large blocks, 87 in small ones).
+    // In fp32 the large one has no registers left.
+    if constexpr (!FP32) {
+        const int large = (blocks_of(a, 16, 16) + 255) / 256, small = (blocks_of(a, 8, 8) + 511) / 512;
+        if (large * 100 <= small * 54) return launch_block<8, 4, 2, 4, FP32>(a, s);
+    }
+    launch_block<4, 4, 2, 2, FP32>(a, s);
 }
 
 }  // namespace

@@ -163,7 +163,7 @@ def test_two_streams_at_once(rows):
 @BOTH
 def test_timer_sees_the_launches(dtype):
     m = B.ScaledMatrix(_randn((100, 256), dtype, 2))
-    few, many = _randn((9, 256), dtype, 1), _randn((90, 256), dtype, 1)
+    few, many = _randn((32, 256), dtype, 1), _randn((90, 256), dtype, 1)
     m.product(few), m.product(many)
     torch.cuda.synchronize()
     B.profile_enable(True, dtype)
