@@ -22,40 +22,51 @@ int check_moe(const duo_moe_config* c) {
 size_t matrix_bytes(const duo_moe_config* c, int N, int K) { return c->scaled ? Narrow::bytes(N, K) : Wide::bytes(N, K); }
 size_t expert_bytes(const duo_moe_config* c) { return 2 * matrix_bytes(c, c->d_ff, c->d_model) + matrix_bytes(c, c->d_model, c->d_ff); }
 
+int up128(int n) { return (n + 127) / 128 * 128; }
+
 struct MoeLayout {  // of the workspace
-    size_t chosen, share, lists, logits, hidden, total;
-    int ff_pad;
+    size_t chosen, share, logits, packed, hidden, partial, total;
 };
 MoeLayout layout_of(const duo_moe_config* c, int rows) {
     MoeLayout l{};
     size_t at = 0;
     const size_t entries = (size_t)rows * c->top_k;
-    l.ff_pad = c->d_ff;
     l.chosen = at, at += up16(4 * entries);
     l.share = at, at += up16(4 * entries);
-    l.lists = at, at += up16(4 * MoeLists::words(moe_most(c->n_experts, rows, c->top_k)));
     l.logits = at, at += up16(8 * (size_t)rows * c->n_experts);
-    l.hidden = at, at += up16(4 * entries * l.ff_pad);
+    l.packed = at, at += 2 * (size_t)rows * up128(c->d_model);
+    l.hidden = at, at += 4 * entries * up128(c->d_ff);
+    l.partial = at, at += rows > MOE_FEW_ROWS ? 4 * entries * c->d_model : 0;
     l.total = at;
     return l;
 }
 
-template <class W, int MT>
-void launch_products(const MoeArgs& a, int most, hipStream_t s) {
-    constexpr int NW = MT > 2 ? 4 : 8;
+int most_active(const MoeArgs& a) { return a.n_experts < a.rows * a.top ? a.n_experts : a.rows * a.top; }
+
+template <class W, int MT, int NW, int PF>
+void launch_gate_up(const MoeArgs& a, hipStream_t s) {
     duo_internal_prof(DUO_PROF_MOE_GATEUP);
-    DUO_LAUNCH((moe_gate_up_kernel<W, MT, NW>), dim3(a.ff / 16, most), dim3(64 * NW), s, a);
+    DUO_LAUNCH((moe_gate_up_kernel<W, MT, NW, PF>), dim3(a.ff / 16, most_active(a)), dim3(64 * NW), s, a);
+}
+template <class W, int MT, int NB, int NW, int PF>
+void launch_down(const MoeArgs& a, hipStream_t s) {
     duo_internal_prof(DUO_PROF_MOE_DOWN);
-    DUO_LAUNCH((moe_down_kernel<W, MT, 8>), dim3(a.d / 16), dim3(512), s, a);
+    DUO_LAUNCH((moe_down_kernel<W, MT, NB, NW, PF>), dim3(a.d / 16 / NB, most_active(a)), dim3(64 * NW), s, a);
+    duo_internal_prof(DUO_PROF_MOE_DOWN);
+    DUO_LAUNCH(moe_combine_kernel, dim3((a.d + 1023) / 1024, a.rows), dim3(256), s, a);
 }
 template <class W>
-void launch_products(const MoeArgs& a, int most, hipStream_t s) {
-    switch ((a.rows + 15) / 16) {
-        case 1: return launch_products<W, 1>(a, most, s);
-        case 2: return launch_products<W, 2>(a, most, s);
-        case 3: return launch_products<W, 3>(a, most, s);
-        case 4: return launch_products<W, 4>(a, most, s);
-        default: return launch_products<W, 5>(a, most, s);
+void launch_products(const MoeArgs& a, hipStream_t s) {
+    if (a.rows <= MOE_FEW_ROWS) {
+        launch_gate_up<W, 1, 8, 2>(a, s);
+        duo_internal_prof(DUO_PROF_MOE_DOWN);
+        DUO_LAUNCH((moe_down_few_kernel<W, 8, 2>), dim3(a.d / 16), dim3(512), s, a);
+    } else if (a.rows * a.top <= 24 * a.n_experts) {  // hardly an expert has more than 32 rows
+        launch_gate_up<W, 2, 4, 2>(a, s);
+        launch_down<W, 2, 2, 4, 2>(a, s);
+    } else {
+        launch_gate_up<W, 5, 4, 2>(a, s);
+        launch_down<W, 5, 2, 4, 1>(a, s);
     }
 }
 
@@ -104,22 +115,28 @@ extern "C" int duo_moe_layer(const duo_moe_config* cfg, const uint16_t* router, 
     char* const ws = static_cast<char*>(workspace);
     MoeArgs a{};
     a.x = x, a.y = y, a.router = router, a.experts = static_cast<const uint8_t*>(experts), a.position = position;
-    a.chosen = chosen ? chosen : reinterpret_cast<int32_t*>(ws + lay.chosen);
-    a.share = share ? share : reinterpret_cast<float*>(ws + lay.share);
-    a.lists = reinterpret_cast<int32_t*>(ws + lay.lists);
+    a.chosen_out = chosen, a.share_out = share;
+    a.chosen = reinterpret_cast<int32_t*>(ws + lay.chosen);
+    a.share = reinterpret_cast<float*>(ws + lay.share);
     a.logits = reinterpret_cast<double*>(ws + lay.logits);
+    a.packed = reinterpret_cast<u16*>(ws + lay.packed);
     a.hidden = reinterpret_cast<u16*>(ws + lay.hidden);
+    a.partial = reinterpret_cast<float*>(ws + lay.partial);
     a.x_stride = x_stride, a.y_stride = y_stride;
     a.expert_bytes = expert_bytes(cfg), a.up_at = matrix_bytes(cfg, cfg->d_ff, d), a.down_at = 2 * a.up_at;
-    a.rows = rows, a.d = d, a.ff = cfg->d_ff, a.ff_pad = lay.ff_pad, a.n_experts = cfg->n_experts, a.top = cfg->top_k, a.renormalise = cfg->renormalise;
+    a.rows = rows, a.d = d, a.d_pad = up128(d), a.ff = cfg->d_ff, a.ff_pad = up128(cfg->d_ff), a.n_experts = cfg->n_experts, a.top = cfg->top_k;
+    a.renormalise = cfg->renormalise;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // not of an earlier call
+    const bool inside = (int64_t)a.n_experts * d <= 524288;
+    if (!inside) {
+        duo_internal_prof(DUO_PROF_MOE_ROUTER);
+        DUO_LAUNCH(moe_logits_kernel, dim3((a.n_experts + 15) / 16, rows), dim3(256), s, a);
+    }
     duo_internal_prof(DUO_PROF_MOE_ROUTER);
-    DUO_LAUNCH(moe_logits_kernel, dim3((a.n_experts + 3) / 4, rows), dim3(256), s, a);
-    duo_internal_prof(DUO_PROF_MOE_ROUTER);
-    DUO_LAUNCH(moe_select_kernel, dim3(1), dim3(1024), s, a);
-    const int most = moe_most(a.n_experts, rows, a.top);
-    if (cfg->scaled) launch_products<Narrow>(a, most, s);
-    else launch_products<Wide>(a, most, s);
+    if (inside) DUO_LAUNCH((moe_router_kernel<true>), dim3(rows), dim3(1024), s, a);
+    else DUO_LAUNCH((moe_router_kernel<false>), dim3(rows), dim3(1024), s, a);
+    if (cfg->scaled) launch_products<Narrow>(a, s);
+    else launch_products<Wide>(a, s);
     return duo_internal_hip_ok(hipGetLastError(), "duo_moe_layer");
 }
