@@ -460,6 +460,7 @@ int duo_scaled_gemm(const uint16_t *x, int64_t x_stride, const void *w, void *y,
  */
 #define DUO_MOE_MAX_EXPERTS 512
 #define DUO_MOE_MAX_TOP     16
+#define DUO_MOE_MAX_STRIDE  8388608 /* elements from row to row */
 typedef struct duo_moe_config {
     int32_t d_model;     /* a multiple of 64, at most 8192 */
     int32_t d_ff;        /* a multiple of 32, at most DUO_SCALED_MAX_K */
@@ -538,7 +539,7 @@ int duo_stream_read_probe(const void *src, size_t bytes, uint32_t *sink, int sin
 #define DUO_PROF_SCALED     12 /* duo_scaled_gemm */
 #define DUO_PROF_MOE_ROUTER 13 /* duo_moe_layer: logits, choice of experts */
 #define DUO_PROF_MOE_GATEUP 14 /* duo_moe_layer: gate/up products + SwiGLU */
-#define DUO_PROF_MOE_DOWN   15 /* duo_moe_layer: down product */
+#define DUO_PROF_MOE_DOWN   15 /* duo_moe_layer: down product, sum over a row's experts */
 #define DUO_PROF_CLASSES    16
 int duo_profile_enable(int enable);
 int duo_profile_read(double *ms, int32_t *launches);

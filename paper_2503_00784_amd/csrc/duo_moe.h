@@ -7,7 +7,6 @@
 #include "duo_e4m3.h"
 
 constexpr int MOE_MAX_EXPERTS = 512, MOE_MAX_TOP = 16, MOE_MAX_ROWS = 80;
-constexpr int MOE_MASK_WORDS = 3;  // bits of 80 rows
 
 struct MoeArgs {
     const u16* x;       // [rows][d]
@@ -20,83 +19,76 @@ struct MoeArgs {
     // workspace
     int32_t* chosen;    // [rows][top], -1 where a row is left out
     float* share;       // [rows][top]
-    double* logits;     // [rows][experts], where a kernel of its own forms them
-    u16* packed;        // [rows][d_pad]: x, zeros behind d
+    double* logits;     // [logit_parts][rows][experts]
     u16* hidden;        // [rows * top][2][ff_pad]: bf16 pairs, zeros behind ff
     float* partial;     // [rows * top][d]: outputs in front of the sum over a row's experts
     int64_t x_stride, y_stride;
     size_t expert_bytes, up_at, down_at;  // bytes of an expert, of what lies in front of its up and down matrices
-    int rows, d, d_pad, ff, ff_pad, n_experts, top, renormalise;
+    int rows, d, ff, ff_pad, n_experts, top, renormalise;
 };
 
 // ---- router.  Logits in 64 bits: which of two experts with nearly equal logits a row takes decides its whole output, and must not hang on the order
-// of a sum.  A wave forms those of four experts for one row: 64 lanes x 8 columns at a time, then a butterfly over the lanes.
-__device__ __forceinline__ void router_logits(const MoeArgs& a, const u16* x, int e0, int lane, double (&sum)[4]) {
+// of a sum.  16 experts x 16 rows a workgroup, by the 64-bit matrix instruction (16 x 16 x 4): it leaves one conversion to 64 bits a lane and operand
+// for 1024 products, where a loop over the columns has one for every product or four, and no sums over lanes.  A lane's eight consecutive columns of
+// a 16-byte load go into eight instructions, which wait for each other; so the columns are spread over up to 64 waves in 16 workgroups (one workgroup
+// of 16 waves: 7.4 us for one row of 2048 columns and 64 experts), whose sums moe_choice_kernel adds.  How they are spread follows from the number of
+// columns alone: a row's logits are the same bits whoever its neighbours are.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr int LOGIT_WAVES = 4;
+__host__ __device__ inline int logit_parts(int d) { return d >= 2048 ? 16 : (d + 127) / 128; }
+__global__ __launch_bounds__(64 * LOGIT_WAVES) void moe_logits_kernel(MoeArgs a) {
+    __shared__ double part[LOGIT_WAVES][4][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int e0 = blockIdx.y * 16, t0 = blockIdx.z * 16;
+    // experts and rows behind the last: the last one again, for nothing; rows that are left out are not read
+    const u16* r = a.router + (size_t)min(e0 + c, a.n_experts - 1) * a.d + 8 * g;
+    const int t = min(t0 + c, a.rows - 1);
+    const bool live = !(a.position && a.position[t] < 0);
+    const u16* x = a.x + (int64_t)t * a.x_stride + 8 * g;
+    f64x4 sum = {0.0, 0.0, 0.0, 0.0};
+    for (int k = 32 * (blockIdx.x * LOGIT_WAVES + wave); k < a.d; k += 32 * LOGIT_WAVES * gridDim.x) {
+        Frag8 u, v;
+        u.q = *reinterpret_cast<const u32x4*>(r + k);
+        v.q = live ? *reinterpret_cast<const u32x4*>(x + k) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = 0.0;
-    const u16* r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = a.router + (size_t)min(e0 + i, a.n_experts - 1) * a.d;
-    for (int k = lane * 8; k < a.d; k += 512) {
-        Frag8 u, v[4];
-        u.q = *reinterpret_cast<const u32x4*>(x + k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i].q = *reinterpret_cast<const u32x4*>(r[i] + k);
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const double f = (double)elem_to_f32(u.h[n]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = fma(f, (double)elem_to_f32(v[i].h[n]), sum[i]);
-        }
+        for (int n = 0; n < 8; ++n) sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)elem_to_f32(u.h[n]), (double)elem_to_f32(v.h[n]), sum, 0, 0, 0);
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], o, 64);
+    for (int i = 0; i < 4; ++i) part[wave][i][lane] = sum[i];
+    __syncthreads();
+    // wave i, register i of its lanes: expert 4 i + g, row c
+    const double s = part[0][wave][lane] + part[1][wave][lane] + part[2][wave][lane] + part[3][wave][lane];
+    const int e = e0 + 4 * wave + g;
+    if (e < a.n_experts && t0 + c < a.rows) a.logits[((size_t)blockIdx.x * a.rows + t0 + c) * a.n_experts + e] = s;
 }
 
-__global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs a) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int e0 = (blockIdx.x * 4 + wave) * 4, t = blockIdx.y;
-    if (e0 >= a.n_experts || (a.position && a.position[t] < 0)) return;
-    double sum[4];
-    router_logits(a, a.x + (int64_t)t * a.x_stride, e0, lane, sum);
-    if (lane == 0)
-        for (int i = 0; i < 4 && e0 + i < a.n_experts; ++i) a.logits[(size_t)t * a.n_experts + e0 + i] = sum[i];
-}
-
-// One workgroup a row: logits (INSIDE: formed here), the rank of every expert, which is the number of experts in front of it (so that all are found
-// at once: no search of top_k rounds), shares, and the row's copy for the products.  NaN counts as the least of values; equal ones rank by their number.
-template <bool INSIDE>
-__global__ __launch_bounds__(1024) void moe_router_kernel(MoeArgs a) {
+// One workgroup a row: its logits' parts added up, the rank of every expert, which is the number of experts in front of it (all at once: no search of top_k
+// rounds), and the shares.  NaN counts as the least of values; equal ones rank by their number.
+constexpr int CHOICE_THREADS = 512;
+__global__ __launch_bounds__(CHOICE_THREADS) void moe_choice_kernel(MoeArgs a) {
     __shared__ double raw[MOE_MAX_EXPERTS], key[MOE_MAX_EXPERTS];
     __shared__ int rank[MOE_MAX_EXPERTS], order[MOE_MAX_TOP];
+    static_assert(CHOICE_THREADS >= MOE_MAX_EXPERTS, "a thread for every expert");
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, t = blockIdx.x, n = a.n_experts;
     if (a.position && a.position[t] < 0) {
         if (tid < a.top) a.chosen[t * a.top + tid] = -1;
         return;
     }
-    const u16* x = a.x + (int64_t)t * a.x_stride;
-    for (int k = tid * 8; k < a.d_pad; k += 8192)
-        *reinterpret_cast<u32x4*>(a.packed + (size_t)t * a.d_pad + k) = k < a.d ? *reinterpret_cast<const u32x4*>(x + k) : u32x4{0u, 0u, 0u, 0u};
-    const double lowest = -__builtin_huge_val();
-    if constexpr (INSIDE) {
-        for (int e0 = 4 * wave; e0 < n; e0 += 64) {
-            double sum[4];
-            router_logits(a, x, e0, lane, sum);
-            if (lane == 0)
-                for (int i = 0; i < 4 && e0 + i < n; ++i) raw[e0 + i] = sum[i], key[e0 + i] = sum[i] == sum[i] ? sum[i] : lowest;
-        }
-    } else if (tid < n) {
-        const double l = a.logits[(size_t)t * n + tid];
-        raw[tid] = l, key[tid] = l == l ? l : lowest;
+    if (tid < n) {
+        double parts[16], l = 0.0;
+        const int n_parts = logit_parts(a.d);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) parts[i] = a.logits[((size_t)min(i, n_parts - 1) * a.rows + t) * n + tid];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) l += i < n_parts ? parts[i] : 0.0;
+        raw[tid] = l, key[tid] = l == l ? l : -__builtin_huge_val();
+        rank[tid] = 0;
     }
-    if (tid < MOE_MAX_EXPERTS) rank[tid] = 0;
     __syncthreads();
     // thread (e, part): the experts of a part of the list that stand in front of e
-    int width = 32;
-    while (width < n) width *= 2;
-    const int e = tid & (width - 1), parts = 1024 / width, each = (n + parts - 1) / parts, first = tid / width * each, last = min(first + each, n);
+    int shift = 5;
+    while (1 << shift < n) ++shift;
+    const int parts = CHOICE_THREADS >> shift, e = tid & ((1 << shift) - 1), each = (n + parts - 1) / parts, first = (tid >> shift) * each, last = min(first + each, n);
     if (e < n) {
         const double mine = key[e];
         int ahead = 0;
@@ -125,60 +117,51 @@ __global__ __launch_bounds__(1024) void moe_router_kernel(MoeArgs a) {
     }
 }
 
-// The rows of the workgroup's expert: number `at` among those that a row has chosen, in ascending order; -1 if there are fewer.  Every workgroup finds
-// them for itself from the list of choices, at most 1280 words out of the caches: cheaper than a launch between the router and the products.
+// What the waves of a workgroup have written to LDS, and nothing else, is there for all of them; loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The expert of the workgroups at place `at` of the grid: the expert of that number or, where the rows make fewer choices than there are experts, that of
+// choice number `at` (-1 if its row is left out).  The same for every lane.
+__device__ __forceinline__ int expert_at(const MoeArgs& a, int at) { return a.rows * a.top < a.n_experts ? __builtin_amdgcn_readfirstlane(a.chosen[at]) : at; }
+
+// The rows that chose it.  Every workgroup finds them for itself from the list of choices, at most 1280 words out of the caches, which costs less than
+// a launch that makes lists.  Their order is left to the atomics: each is a column of its own in the products, and comes out the same wherever it stands.
 struct ExpertRows {
-    uint32_t used[MOE_MAX_EXPERTS / 32], mask[MOE_MASK_WORDS];
-    int16_t entry[MOE_MAX_ROWS];  // row * top + place, in ascending order
+    int count, first;             // first: the first choice of the expert
+    int16_t entry[MOE_MAX_ROWS];  // row * top + place
 };
+// false: nothing to do here, no row chose the expert or the workgroups of an earlier choice have it
 template <int THREADS>
-__device__ __forceinline__ int find_expert(const MoeArgs& a, ExpertRows& r, int at, int& count) {
+__device__ __forceinline__ bool find_rows(const MoeArgs& a, ExpertRows& r, int at, int e) {
     constexpr int EACH = (MOE_MAX_ROWS * MOE_MAX_TOP + THREADS - 1) / THREADS;
     const int tid = threadIdx.x, entries = a.rows * a.top;
+    if (a.rows == 1 && entries < a.n_experts) {  // choice `at` is the only one of its expert
+        if (tid == 0) r.count = 1, r.entry[0] = (int16_t)at;
+        lds_barrier();
+        return true;
+    }
     int chosen[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) chosen[i] = i * THREADS + tid < entries ? a.chosen[i * THREADS + tid] : -1;
-    for (int i = tid; i < MOE_MAX_EXPERTS / 32 + MOE_MASK_WORDS; i += THREADS) (i < MOE_MAX_EXPERTS / 32 ? r.used[i] : r.mask[i - MOE_MAX_EXPERTS / 32]) = 0u;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < EACH; ++i)
-        if (chosen[i] >= 0) atomicOr(&r.used[chosen[i] >> 5], 1u << (chosen[i] & 31));
-    __syncthreads();
-    int e = -1, left = at;
-    for (int w = 0; w < MOE_MAX_EXPERTS / 32; ++w) {
-        uint32_t bits = r.used[w];
-        const int here = __popc(bits);
-        if (left < here && e < 0) {
-            for (int i = 0; i < left; ++i) bits &= bits - 1u;
-            e = 32 * w + __ffs(bits) - 1;
-        }
-        left -= here;
-    }
-    e = __builtin_amdgcn_readfirstlane(e);
-    if (e < 0) return -1;
+    if (tid == 0) r.count = 0, r.first = 0x7fffffff;
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
         if (chosen[i] == e) {
-            const int t = (i * THREADS + tid) / a.top;
-            atomicOr(&r.mask[t >> 5], 1u << (t & 31));
+            r.entry[atomicAdd(&r.count, 1)] = (int16_t)(i * THREADS + tid);
+            atomicMin(&r.first, i * THREADS + tid);
         }
-    __syncthreads();
-    count = __builtin_amdgcn_readfirstlane(__popc(r.mask[0]) + __popc(r.mask[1]) + __popc(r.mask[2]));
-#pragma unroll
-    for (int i = 0; i < EACH; ++i)
-        if (chosen[i] == e) {
-            const int t = (i * THREADS + tid) / a.top;
-            int n = __popc(r.mask[t >> 5] & ((1u << (t & 31)) - 1u));
-            for (int w = 0; w < t >> 5; ++w) n += __popc(r.mask[w]);
-            r.entry[n] = (int16_t)(i * THREADS + tid);
-        }
-    __syncthreads();
-    return e;
+    lds_barrier();
+    return r.count > 0 && (entries >= a.n_experts || r.first == at);
 }
 
 // Rows are read through buffer descriptors: lanes without a row ask for an offset behind the end and get zeros without a memory access, and the
-// loop has no branch around its loads, so that the compiler can count them.  Offsets stay below 2^31 (80 rows x 16 experts x 65536 channels x 4
-// bytes are 2^28.4).
+// loop has no branch around its loads, so that the compiler can count them.  Offsets stay below 2^31: 80 rows x 16 experts x 65536 channels x 4
+// bytes are 2^28.4, 80 rows at the largest distance of 2^23 elements 2^30.4.
 constexpr uint32_t NO_ROW = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, size_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (uint32_t)bytes, 0x00027000);
@@ -259,39 +242,49 @@ __global__ __launch_bounds__(64 * NW) void moe_gate_up_kernel(MoeArgs a) {
     __shared__ f32x4 part[NW][2 * MT][64];
     __shared__ ExpertRows rows;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int band = blockIdx.x, KB = a.d_pad >> 7, n = (KB - wave + NW - 1) / NW;
-    int count = 0;
-    const int e = find_expert<64 * NW>(a, rows, blockIdx.y, count);
+    const int band = blockIdx.x, KB = (a.d + 127) >> 7, n = (KB - wave + NW - 1) / NW;
+    const int e = expert_at(a, blockIdx.y);
     if (e < 0) return;
     const uint8_t* gate = a.experts + (size_t)e * a.expert_bytes;
     const uint8_t* up = gate + a.up_at;
-    const __amdgpu_buffer_rsrc_t xs = row_buffer(a.packed, (size_t)a.rows * a.d_pad * 2);
+    W w[PF][2];
+    auto block = [&](int i) { return max(min(wave + NW * min(i, n - 1), KB - 1), 0); };
+    auto load_weights = [&](int s, int i) {
+        w[s][0].load(gate, a.ff, a.d, band, block(i), lane);
+        w[s][1].load(up, a.ff, a.d, band, block(i), lane);
+    };
+    if (!find_rows<64 * NW>(a, rows, blockIdx.y, e)) return;
+    const int count = __builtin_amdgcn_readfirstlane(rows.count);
+    const __amdgpu_buffer_rsrc_t xs = row_buffer(a.x, ((size_t)(a.rows - 1) * a.x_stride + a.d) * 2);
     for (int first = 0; first < count; first += 16 * MT) {
         uint32_t row[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int i = first + m * 16 + c;
-            row[m] = i < count ? (uint32_t)(rows.entry[i] / a.top) * a.d_pad * 2 : NO_ROW;
+            row[m] = i < count ? (uint32_t)(rows.entry[i] / a.top) * (uint32_t)a.x_stride * 2 : NO_ROW;
         }
         f32x4 acc[2][MT];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[b][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-        W w[PF][2];
         u32x4 x[PF][MT][4];
-        auto load = [&](int s, int i) {
-            const int j = max(min(wave + NW * min(i, n - 1), KB - 1), 0);
-            w[s][0].load(gate, a.ff, a.d, band, j, lane);
-            w[s][1].load(up, a.ff, a.d, band, j, lane);
+        auto load_rows = [&](int s, int i) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[s][m][q] = row_load(xs, row[m] + (uint32_t)(j * 128 + W::column(q, g)) * 2);
+                for (int q = 0; q < 4; ++q) x[s][m][q] = row_load(xs, row[m] + (uint32_t)(block(i) * 128 + W::column(q, g)) * 2);
         };
         auto products = [&](int s, int i) {
             const int j = wave + NW * i;
-            if ((j + 1) * 128 > a.d) w[s][0].cut(a.d, j), w[s][1].cut(a.d, j);
+            if ((j + 1) * 128 > a.d) {  // columns from d on: zeros, whatever lies behind the rows
+                w[s][0].cut(a.d, j), w[s][1].cut(a.d, j);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (j * 128 + W::column(q, g) >= a.d) x[s][m][q] = u32x4{0u, 0u, 0u, 0u};
+            }
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 elem8 o[4];
@@ -308,13 +301,14 @@ __global__ __launch_bounds__(64 * NW) void moe_gate_up_kernel(MoeArgs a) {
             }
         };
 #pragma unroll
-        for (int s = 0; s < PF; ++s) load(s, s);
+        for (int s = 0; s < PF; ++s) load_weights(s, s), load_rows(s, s);
         int i = 0;
         for (; i + PF < n; i += PF) {
 #pragma unroll
             for (int s = 0; s < PF; ++s) {
                 products(s, i + s);
-                load(s, i + s + PF);
+                load_weights(s, i + s + PF);
+                load_rows(s, i + s + PF);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -393,99 +387,27 @@ __device__ __forceinline__ void down_block(f32x4& acc, const W& w, const DownOpe
     add_block(acc, sum, w);
 }
 
-// ---- down, up to 16 rows.  A workgroup owns 16 output channels of all rows; its waves share out (expert, 128 hidden channels) in runs.  The columns
-// of the product are the step's rows, with zeros where a row did not choose the expert, so that all experts add into the same sums and an output is
-// formed in one place.
-constexpr int MOE_FEW_ROWS = 16;
-template <class W, int NW, int PF>
-__global__ __launch_bounds__(64 * NW) void moe_down_few_kernel(MoeArgs a) {
-    __shared__ f32x4 part[NW][64];
-    __shared__ uint32_t used[MOE_MAX_EXPERTS / 32];
-    __shared__ int16_t expert[MOE_FEW_ROWS * MOE_MAX_TOP], entry[MOE_FEW_ROWS * MOE_MAX_TOP][MOE_FEW_ROWS];  // of the active experts; -1: not chosen
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, tid = threadIdx.x;
-    const int band = blockIdx.x, KB = a.ff_pad >> 7, entries = a.rows * a.top;  // at most 256 entries
-    static_assert(64 * NW >= MOE_FEW_ROWS * MOE_MAX_TOP, "a thread per entry");
-    const int mine = tid < entries ? a.chosen[tid] : -1;
-    if (tid < MOE_MAX_EXPERTS / 32) used[tid] = 0u;
-    for (int i = tid; i < entries * MOE_FEW_ROWS; i += 64 * NW) (&entry[0][0])[i] = -1;
-    __syncthreads();
-    if (mine >= 0) atomicOr(&used[mine >> 5], 1u << (mine & 31));
-    __syncthreads();
-    int active = 0, at = 0;
-    for (int w = 0; w < MOE_MAX_EXPERTS / 32; ++w) {
-        if (w == mine >> 5) at = active + __popc(used[w] & ((1u << (mine & 31)) - 1u));
-        active += __popc(used[w]);
-    }
-    if (mine >= 0) expert[at] = (int16_t)mine, entry[at][tid / a.top] = (int16_t)tid;
-    __syncthreads();
-    active = __builtin_amdgcn_readfirstlane(active);
-    const int items = active * KB, begin = wave * items / NW, end = (wave + 1) * items / NW;  // at most 256 * 512 items
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (begin < end) {
-        const __amdgpu_buffer_rsrc_t hs = row_buffer(a.hidden, (size_t)entries * a.ff_pad * 4);
-        int to_load = begin, la = begin / KB, lj = begin - la * KB, ci = begin - la * KB;  // ci: the block of columns of the next item to compute
-        W w[PF];
-        u32x4 x[PF][8];
-        auto load = [&](int s) {
-            const int e = __builtin_amdgcn_readfirstlane(expert[la]), p = entry[la][c];
-            const uint32_t row = p < 0 ? NO_ROW : (uint32_t)p * a.ff_pad * 4;
-            w[s].load(a.experts + (size_t)e * a.expert_bytes + a.down_at, a.d, a.ff, band, lj, lane);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t k = (uint32_t)(lj * 128 + W::column(q, g)) * 2;
-                x[s][q] = row_load(hs, row + k);
-                x[s][4 + q] = row_load(hs, row + (uint32_t)a.ff_pad * 2 + k);
-            }
-            if (to_load + 1 < end) {  // the last one again where there is none
-                ++to_load;
-                if (++lj == KB) lj = 0, ++la;
-            }
-        };
-        auto products = [&](int s) {
-            if ((ci + 1) * 128 > a.ff) w[s].cut(a.ff, ci);
-            if (++ci == KB) ci = 0;
-            const DownOperand<W> o[4] = {DownOperand<W>(w[s], 0), DownOperand<W>(w[s], 1), DownOperand<W>(w[s], 2), DownOperand<W>(w[s], 3)};
-            down_block(acc, w[s], o, x[s]);
-        };
-#pragma unroll
-        for (int s = 0; s < PF; ++s) load(s);
-        int i = begin;
-        for (; i + PF < end; i += PF) {
-#pragma unroll
-            for (int s = 0; s < PF; ++s) {
-                products(s);
-                load(s);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-#pragma unroll
-        for (int s = 0; s < PF; ++s)
-            if (i + s < end) products(s);
-    }
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0) {
-        f32x4 v = part[0][lane];
-        for (int w = 1; w < NW; ++w) v += part[w][lane];
-        if (c < a.rows && !(a.position && a.position[c] < 0)) {
-            u16* y = a.y + (int64_t)c * a.y_stride + band * 16 + 4 * g;
-            *reinterpret_cast<uint2*>(y) = make_uint2(pack_elem2(v[0], v[1]), pack_elem2(v[2], v[3]));
-        }
-    }
-}
-
-// ---- down, more rows.  As gate and up: a workgroup owns NB bands of one expert, the columns are the rows that chose it; what a row gets from each of
-// its experts is left apart in fp32 and added up by moe_combine_kernel in the order of its choices.
+// ---- down.  As gate and up: a workgroup owns NB bands of one expert, the columns are the rows that chose it; what a row gets from each of its experts
+// is left apart in fp32 and added up by moe_combine_kernel in the order of its choices.  (One workgroup for 16 outputs of all rows and all experts
+// needs neither, but then a few hundred workgroups read everything, 16 columns at a time: 16 rows on 50 active experts of 2048 x 1408 in 8 bits 62 us,
+// 27 + 4 like this; one row on 6 in 16 bits 12.5, 8.5 + 3.)
 template <class W, int MT, int NB, int NW, int PF>
 __global__ __launch_bounds__(64 * NW) void moe_down_kernel(MoeArgs a) {
     __shared__ f32x4 part[NW][NB * MT][64];
     __shared__ ExpertRows rows;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int band0 = blockIdx.x * NB, KB = a.ff_pad >> 7, n = (KB - wave + NW - 1) / NW;  // d is a multiple of 64: NB divides its bands
-    int count = 0;
-    const int e = find_expert<64 * NW>(a, rows, blockIdx.y, count);
+    const int e = expert_at(a, blockIdx.y);
     if (e < 0) return;
     const uint8_t* down = a.experts + (size_t)e * a.expert_bytes + a.down_at;
+    W w[PF][NB];
+    auto block = [&](int i) { return max(min(wave + NW * min(i, n - 1), KB - 1), 0); };
+    auto load_weights = [&](int s, int i) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) w[s][b].load(down, a.d, a.ff, band0 + b, block(i), lane);
+    };
+    if (!find_rows<64 * NW>(a, rows, blockIdx.y, e)) return;
+    const int count = __builtin_amdgcn_readfirstlane(rows.count);
     const __amdgpu_buffer_rsrc_t hs = row_buffer(a.hidden, (size_t)a.rows * a.top * a.ff_pad * 4);
     for (int first = 0; first < count; first += 16 * MT) {
         uint32_t row[MT];
@@ -499,17 +421,13 @@ __global__ __launch_bounds__(64 * NW) void moe_down_kernel(MoeArgs a) {
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[b][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-        W w[PF][NB];
         u32x4 x[PF][MT][8];
-        auto load = [&](int s, int i) {
-            const int j = max(min(wave + NW * min(i, n - 1), KB - 1), 0);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) w[s][b].load(down, a.d, a.ff, band0 + b, j, lane);
+        auto load_rows = [&](int s, int i) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint32_t k = (uint32_t)(j * 128 + W::column(q, g)) * 2;
+                    const uint32_t k = (uint32_t)(block(i) * 128 + W::column(q, g)) * 2;
                     x[s][m][q] = row_load(hs, row[m] + k);
                     x[s][m][4 + q] = row_load(hs, row[m] + (uint32_t)a.ff_pad * 2 + k);
                 }
@@ -526,13 +444,14 @@ __global__ __launch_bounds__(64 * NW) void moe_down_kernel(MoeArgs a) {
             }
         };
 #pragma unroll
-        for (int s = 0; s < PF; ++s) load(s, s);
+        for (int s = 0; s < PF; ++s) load_weights(s, s), load_rows(s, s);
         int i = 0;
         for (; i + PF < n; i += PF) {
 #pragma unroll
             for (int s = 0; s < PF; ++s) {
                 products(s, i + s);
-                load(s, i + s + PF);
+                load_weights(s, i + s + PF);
+                load_rows(s, i + s + PF);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -559,7 +478,14 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(MoeArgs a) {
     const int t = blockIdx.y, k = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (k >= a.d || (a.position && a.position[t] < 0)) return;
     const float* p = a.partial + (size_t)t * a.top * a.d + k;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.top; ++j) v += *reinterpret_cast<const f32x4*>(p + (size_t)j * a.d);
+    f32x4 v = *reinterpret_cast<const f32x4*>(p);
+    for (int j = 1; j < a.top; j += 4) {  // four loads at a time
+        f32x4 u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(p + (size_t)min(j + i, a.top - 1) * a.d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (j + i < a.top) v += u[i];
+    }
     *reinterpret_cast<uint2*>(a.y + (int64_t)t * a.y_stride + k) = make_uint2(pack_elem2(v[0], v[1]), pack_elem2(v[2], v[3]));
 }

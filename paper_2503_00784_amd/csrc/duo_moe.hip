@@ -25,7 +25,7 @@ size_t expert_bytes(const duo_moe_config* c) { return 2 * matrix_bytes(c, c->d_f
 int up128(int n) { return (n + 127) / 128 * 128; }
 
 struct MoeLayout {  // of the workspace
-    size_t chosen, share, logits, packed, hidden, partial, total;
+    size_t chosen, share, logits, hidden, partial, total;
 };
 MoeLayout layout_of(const duo_moe_config* c, int rows) {
     MoeLayout l{};
@@ -33,10 +33,9 @@ MoeLayout layout_of(const duo_moe_config* c, int rows) {
     const size_t entries = (size_t)rows * c->top_k;
     l.chosen = at, at += up16(4 * entries);
     l.share = at, at += up16(4 * entries);
-    l.logits = at, at += up16(8 * (size_t)rows * c->n_experts);
-    l.packed = at, at += 2 * (size_t)rows * up128(c->d_model);
+    l.logits = at, at += up16(8 * (size_t)rows * c->n_experts * logit_parts(c->d_model));
     l.hidden = at, at += 4 * entries * up128(c->d_ff);
-    l.partial = at, at += rows > MOE_FEW_ROWS ? 4 * entries * c->d_model : 0;
+    l.partial = at, at += 4 * entries * c->d_model;
     l.total = at;
     return l;
 }
@@ -55,18 +54,24 @@ void launch_down(const MoeArgs& a, hipStream_t s) {
     duo_internal_prof(DUO_PROF_MOE_DOWN);
     DUO_LAUNCH(moe_combine_kernel, dim3((a.d + 1023) / 1024, a.rows), dim3(256), s, a);
 }
+// By the rows an expert has where all have as many.  Up to 12 hardly an expert has more than 16, and one tile of rows it is, twice over a matrix where
+// one has: 80 rows, two choices of 8 experts (20 each) 102 us like this, 68 with two tiles; of 16 (10 each) 50, 52.  40 rows each: two tiles 29 us,
+// three 21, five 22.
 template <class W>
 void launch_products(const MoeArgs& a, hipStream_t s) {
-    if (a.rows <= MOE_FEW_ROWS) {
-        launch_gate_up<W, 1, 8, 2>(a, s);
-        duo_internal_prof(DUO_PROF_MOE_DOWN);
-        DUO_LAUNCH((moe_down_few_kernel<W, 8, 2>), dim3(a.d / 16), dim3(512), s, a);
-    } else if (a.rows * a.top <= 24 * a.n_experts) {  // hardly an expert has more than 32 rows
-        launch_gate_up<W, 2, 4, 2>(a, s);
-        launch_down<W, 2, 2, 4, 2>(a, s);
+    const int each = a.rows * a.top / a.n_experts;
+    if (each <= 12 || a.rows <= 16) {
+        launch_gate_up<W, 1, 4, 2>(a, s);
+        // four bands for two waves where that makes enough workgroups (128 experts of 4096 x 1536 in 8 bits: 145 us, two bands for four waves 171; two
+        // experts of 4096 x 14336: 30, 22)
+        if (most_active(a) * a.d > 16384) launch_down<W, 1, 4, 2, 1>(a, s);
+        else launch_down<W, 1, 2, 4, 2>(a, s);
+    } else if (each <= 28) {
+        launch_gate_up<W, 2, 4, 1>(a, s);
+        launch_down<W, 2, 4, 4, 1>(a, s);
     } else {
-        launch_gate_up<W, 5, 4, 2>(a, s);
-        launch_down<W, 5, 2, 4, 1>(a, s);
+        launch_gate_up<W, 3, 4, 1>(a, s);
+        launch_down<W, 3, 4, 4, 1>(a, s);
     }
 }
 
@@ -109,7 +114,7 @@ extern "C" int duo_moe_layer(const duo_moe_config* cfg, const uint16_t* router, 
     if (off16(router) || off16(experts) || off16(x) || off16(y) || off16(workspace) || x_stride % 8 || y_stride % 8) return DUO_ERR_ALIGN;
     if (off4(position) || off4(chosen) || off4(share)) return DUO_ERR_ALIGN;
     const int d = cfg->d_model;
-    if (rows > 1 && (x_stride < d || y_stride < d || x_stride > DUO_SCALED_MAX_STRIDE || y_stride > DUO_SCALED_MAX_STRIDE)) return DUO_ERR_SHAPE;
+    if (rows > 1 && (x_stride < d || y_stride < d || x_stride > DUO_MOE_MAX_STRIDE || y_stride > DUO_MOE_MAX_STRIDE)) return DUO_ERR_SHAPE;
     const MoeLayout lay = layout_of(cfg, rows);
     if (workspace_bytes < lay.total) return DUO_ERR_WORKSPACE;
     char* const ws = static_cast<char*>(workspace);
@@ -119,23 +124,18 @@ extern "C" int duo_moe_layer(const duo_moe_config* cfg, const uint16_t* router, 
     a.chosen = reinterpret_cast<int32_t*>(ws + lay.chosen);
     a.share = reinterpret_cast<float*>(ws + lay.share);
     a.logits = reinterpret_cast<double*>(ws + lay.logits);
-    a.packed = reinterpret_cast<u16*>(ws + lay.packed);
     a.hidden = reinterpret_cast<u16*>(ws + lay.hidden);
     a.partial = reinterpret_cast<float*>(ws + lay.partial);
     a.x_stride = x_stride, a.y_stride = y_stride;
     a.expert_bytes = expert_bytes(cfg), a.up_at = matrix_bytes(cfg, cfg->d_ff, d), a.down_at = 2 * a.up_at;
-    a.rows = rows, a.d = d, a.d_pad = up128(d), a.ff = cfg->d_ff, a.ff_pad = up128(cfg->d_ff), a.n_experts = cfg->n_experts, a.top = cfg->top_k;
+    a.rows = rows, a.d = d, a.ff = cfg->d_ff, a.ff_pad = up128(cfg->d_ff), a.n_experts = cfg->n_experts, a.top = cfg->top_k;
     a.renormalise = cfg->renormalise;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // not of an earlier call
-    const bool inside = (int64_t)a.n_experts * d <= 524288;
-    if (!inside) {
-        duo_internal_prof(DUO_PROF_MOE_ROUTER);
-        DUO_LAUNCH(moe_logits_kernel, dim3((a.n_experts + 15) / 16, rows), dim3(256), s, a);
-    }
     duo_internal_prof(DUO_PROF_MOE_ROUTER);
-    if (inside) DUO_LAUNCH((moe_router_kernel<true>), dim3(rows), dim3(1024), s, a);
-    else DUO_LAUNCH((moe_router_kernel<false>), dim3(rows), dim3(1024), s, a);
+    DUO_LAUNCH(moe_logits_kernel, dim3(logit_parts(d), (a.n_experts + 15) / 16, (rows + 15) / 16), dim3(64 * LOGIT_WAVES), s, a);
+    duo_internal_prof(DUO_PROF_MOE_ROUTER);
+    DUO_LAUNCH(moe_choice_kernel, dim3(rows), dim3(CHOICE_THREADS), s, a);
     if (cfg->scaled) launch_products<Narrow>(a, s);
     else launch_products<Wide>(a, s);
     return duo_internal_hip_ok(hipGetLastError(), "duo_moe_layer");

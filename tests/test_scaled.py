@@ -122,7 +122,7 @@ def test_layer_refuses(lib):
         assert _layer(lib, rows=rows) == -2
     for bad in BAD_SHAPES:
         assert _layer(lib, _cfg(**bad), nbytes=1 << 40) == -2, bad
-    for bad in ({"xs": 120}, {"ys": 64}, {"xs": 2 ** 31 + 8}, {"ys": -128}):
+    for bad in ({"xs": 120}, {"ys": 64}, {"xs": 2 ** 23 + 8}, {"ys": 2 ** 23 + 8}, {"ys": -128}):
         assert _layer(lib, **bad) == -2, bad
     for bad in ({"router": A + 8}, {"experts": A + 4}, {"x": A + 2}, {"y": A + 8}, {"ws": A + 8}, {"xs": 132}, {"ys": 130}, {"position": A + 2}, {"chosen": A + 1},
                 {"share": A + 3}):
