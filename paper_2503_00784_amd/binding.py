@@ -695,20 +695,20 @@ class _OnDevice:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
         self._element = torch.float16 if dtype == "fp16" else torch.bfloat16
-        # the current stream's pointer without a Stream object, where torch has that (it is no public name)
+        # the current stream's pointer and the current device without what torch's public calls add to them, where torch has that
         self._stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self._current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.lib = load(dtype)
 
-    def _call(self, name: str, *args) -> None:
-        cuda, function = self._torch.cuda, getattr(self.lib, name)
+    def _call(self, function, *args) -> None:
         stream = self._stream_of(self._index)
-        if self._index == cuda.current_device():
+        if self._index == self._current():
             rc = function(*args, stream)
         else:
-            with cuda.device(self._index):
+            with self._torch.cuda.device(self._index):
                 rc = function(*args, stream)
         if rc:
-            _check(rc, name)
+            _check(rc, function.__name__)
 
     def _matrix(self, name: str, w, N: int, K: int):
         """A weight matrix as the packing calls take it: contiguous, of the handle's type, 16-byte aligned."""
@@ -755,9 +755,10 @@ class ScaledMatrix(_OnDevice):
             raise ValueError(f"[{self.N}][{self.K}]: K must be a multiple of 32, at most {SCALED_MAX_K}, N at most {SCALED_MAX_N}")
         w = self._matrix("w", w, self.N, self.K)
         self._bytes = self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
-        self._call("duo_scaled_pack", w.data_ptr(), self.N, self.K, self._bytes.data_ptr())
+        self._call(self.lib.duo_scaled_pack, w.data_ptr(), self.N, self.K, self._bytes.data_ptr())
         self._ptr = self._bytes.data_ptr()
         self._in, self._out = (self._element,), (self._element, self._torch.float32)
+        self._gemm = self.lib.duo_scaled_gemm
 
     @property
     def packed(self):
@@ -794,7 +795,7 @@ class ScaledMatrix(_OnDevice):
             nbytes = need.value
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)  # of this call and its stream
             wp = workspace.data_ptr()
-        self._call("duo_scaled_gemm", xp, xs, self._ptr, yp, ys, 1 if out.dtype == torch.float32 else 0, rows, self.N, self.K, wp, nbytes)
+        self._call(self._gemm, xp, xs, self._ptr, yp, ys, 1 if out.dtype == torch.float32 else 0, rows, self.N, self.K, wp, nbytes)
         return out
 
 
@@ -827,14 +828,14 @@ class ExpertLayer(_OnDevice):
             if taken == n:
                 raise ValueError(f"more than {n} experts, the router's rows")
             m = [self._matrix(name, w, *dims) for name, w, dims in (("gate", gate, (ff, d)), ("up", up, (ff, d)), ("down", down, (d, ff)))]
-            self._call("duo_moe_pack", C.byref(self.cfg), *[w.data_ptr() for w in m], taken, self._packed.data_ptr())
+            self._call(self.lib.duo_moe_pack, C.byref(self.cfg), *[w.data_ptr() for w in m], taken, self._packed.data_ptr())
             taken += 1
         if taken != n or n == 0:
             raise ValueError(f"{taken} experts, the router has {n} rows")
         self.n_experts, self.d_model, self.d_ff, self.top_k = n, d, ff, int(top_k)
         self.scaled, self.renormalise = bool(scaled), bool(renormalise)
         self._ref, self._router_ptr, self._experts_ptr = C.byref(self.cfg), self._router.data_ptr(), self._packed.data_ptr()
-        self._types = (self._element,)
+        self._types, self._layer = (self._element,), self.lib.duo_moe_layer
         self._need = {}  # rows -> bytes of workspace
 
     def _workspace_bytes(self, rows: int) -> int:
@@ -871,7 +872,7 @@ class ExpertLayer(_OnDevice):
             return out, chosen, share
         need = self._workspace_bytes(rows)
         workspace = torch.empty(need, dtype=torch.uint8, device=self.device)  # of this call and its stream
-        self._call("duo_moe_layer", self._ref, self._router_ptr, self._experts_ptr, xp, xs, rows, _ptr(position), yp, ys, chosen.data_ptr(),
+        self._call(self._layer, self._ref, self._router_ptr, self._experts_ptr, xp, xs, rows, _ptr(position), yp, ys, chosen.data_ptr(),
                    share.data_ptr(), workspace.data_ptr(), need)
         return out, chosen, share
 

@@ -117,6 +117,73 @@ __global__ __launch_bounds__(CHOICE_THREADS) void moe_choice_kernel(MoeArgs a) {
     }
 }
 
+// Both in one launch for small routers: a workgroup for 16 rows, whose 16 waves share out (16 experts, part of the columns).  One compute unit has to form
+// all products of 16 rows, a 64-bit instruction every 64 clocks on each of its four matrix units: 4 experts of 768 columns 4.6 us (3.0 + 3.0 in two
+// launches), but 32 experts of 2048 columns 16 us (4.8 + 4.6).
+constexpr int ROUTER_WAVES = 16, ROUTER_EXPERTS = 32;
+__host__ inline bool router_in_one(int experts, int d) { return experts <= ROUTER_EXPERTS && (experts > 16 ? 2 : 1) * d <= 1024; }
+__global__ __launch_bounds__(64 * ROUTER_WAVES) void moe_router_kernel(MoeArgs a) {
+    __shared__ double part[ROUTER_WAVES][4][64], raw[16][ROUTER_EXPERTS];
+    __shared__ int order[16][MOE_MAX_TOP];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, n = a.n_experts;
+    const int tiles = n > 16 ? 2 : 1, tile = wave & (tiles - 1), parts = ROUTER_WAVES / tiles, t0 = blockIdx.x * 16;
+    {
+        const u16* r = a.router + (size_t)min(16 * tile + c, n - 1) * a.d + 8 * g;
+        const int t = min(t0 + c, a.rows - 1);
+        const bool live = !(a.position && a.position[t] < 0);
+        const u16* x = a.x + (int64_t)t * a.x_stride + 8 * g;
+        f64x4 sum = {0.0, 0.0, 0.0, 0.0};
+        for (int k = 32 * (wave / tiles); k < a.d; k += 32 * parts) {
+            Frag8 u, v;
+            u.q = *reinterpret_cast<const u32x4*>(r + k);
+            v.q = live ? *reinterpret_cast<const u32x4*>(x + k) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)elem_to_f32(u.h[i]), (double)elem_to_f32(v.h[i]), sum, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[wave][i][lane] = sum[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < 16 * ROUTER_EXPERTS) {  // register i of lane (c, g): expert 4 i + g of the tile, row c
+        const int row = threadIdx.x & 15, e = threadIdx.x >> 4, w = e >> 4;
+        if (w < tiles) {
+            double s = 0.0;
+            for (int p = 0; p < parts; ++p) s += part[p * tiles + w][(e & 15) >> 2][(e & 3) * 16 + row];
+            raw[row][e] = s;
+        }
+    }
+    __syncthreads();
+    const int t = t0 + wave;  // a wave a row from here on
+    if (t >= a.rows) return;
+    if (a.position && a.position[t] < 0) {
+        if (lane < a.top) a.chosen[t * a.top + lane] = -1;
+        return;
+    }
+    const double lowest = -__builtin_huge_val();
+    const int e = lane & 31;  // the lanes of one half compare with even experts, those of the other with odd ones
+    const double l = raw[wave][min(e, n - 1)], mine = l == l ? l : lowest;
+    int ahead = 0;
+    for (int j = lane >> 5; j < n; j += 2) {
+        const double o = raw[wave][j], other = o == o ? o : lowest;
+        ahead += other > mine || (other == mine && j < e);
+    }
+    ahead += __shfl_xor(ahead, 32, 64);
+    if (lane < n && ahead < a.top) order[wave][ahead] = e;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    const int at = lane < a.top ? order[wave][lane] : 0;
+    const double most = raw[wave][order[wave][0]];
+    const double p = lane < a.top ? exp(raw[wave][at] - most) : 0.0;
+    const double sum = wave_sum(a.renormalise ? p : lane < n ? exp(l - most) : 0.0);
+    if (lane < a.top) {
+        const float share = (float)(p / sum);
+        a.chosen[t * a.top + lane] = at, a.share[t * a.top + lane] = share;
+        if (a.chosen_out) a.chosen_out[t * a.top + lane] = at;
+        if (a.share_out) a.share_out[t * a.top + lane] = share;
+    }
+}
+
 // What the waves of a workgroup have written to LDS, and nothing else, is there for all of them; loads from memory stay on their way.
 __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -391,7 +458,8 @@ __device__ __forceinline__ void down_block(f32x4& acc, const W& w, const DownOpe
 // is left apart in fp32 and added up by moe_combine_kernel in the order of its choices.  (One workgroup for 16 outputs of all rows and all experts
 // needs neither, but then a few hundred workgroups read everything, 16 columns at a time: 16 rows on 50 active experts of 2048 x 1408 in 8 bits 62 us,
 // 27 + 4 like this; one row on 6 in 16 bits 12.5, 8.5 + 3.)
-template <class W, int MT, int NB, int NW, int PF>
+// ONE choice a row: there is nothing to add, and the outputs go where they belong.
+template <class W, int MT, int NB, int NW, int PF, bool ONE>
 __global__ __launch_bounds__(64 * NW) void moe_down_kernel(MoeArgs a) {
     __shared__ f32x4 part[NW][NB * MT][64];
     __shared__ ExpertRows rows;
@@ -467,7 +535,11 @@ __global__ __launch_bounds__(64 * NW) void moe_down_kernel(MoeArgs a) {
             f32x4 v = part[0][t][lane];
             for (int u = 1; u < NW; ++u) v += part[u][t][lane];
             const int at = first + (t % MT) * 16 + c;
-            if (at < count) *reinterpret_cast<f32x4*>(a.partial + (size_t)rows.entry[at] * a.d + (band0 + t / MT) * 16 + 4 * g) = v;
+            if (at < count) {
+                const int p = rows.entry[at], k = (band0 + t / MT) * 16 + 4 * g;
+                if constexpr (ONE) *reinterpret_cast<uint2*>(a.y + (int64_t)p * a.y_stride + k) = make_uint2(pack_elem2(v[0], v[1]), pack_elem2(v[2], v[3]));
+                else *reinterpret_cast<f32x4*>(a.partial + (size_t)p * a.d + k) = v;
+            }
         }
         __syncthreads();
     }

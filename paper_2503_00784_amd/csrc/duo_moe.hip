@@ -35,7 +35,7 @@ MoeLayout layout_of(const duo_moe_config* c, int rows) {
     l.share = at, at += up16(4 * entries);
     l.logits = at, at += up16(8 * (size_t)rows * c->n_experts * logit_parts(c->d_model));
     l.hidden = at, at += 4 * entries * up128(c->d_ff);
-    l.partial = at, at += 4 * entries * c->d_model;
+    l.partial = at, at += c->top_k > 1 ? 4 * entries * c->d_model : 0;
     l.total = at;
     return l;
 }
@@ -49,8 +49,13 @@ void launch_gate_up(const MoeArgs& a, hipStream_t s) {
 }
 template <class W, int MT, int NB, int NW, int PF>
 void launch_down(const MoeArgs& a, hipStream_t s) {
+    const dim3 grid(a.d / 16 / NB, most_active(a));
     duo_internal_prof(DUO_PROF_MOE_DOWN);
-    DUO_LAUNCH((moe_down_kernel<W, MT, NB, NW, PF>), dim3(a.d / 16 / NB, most_active(a)), dim3(64 * NW), s, a);
+    if (a.top == 1) {
+        DUO_LAUNCH((moe_down_kernel<W, MT, NB, NW, PF, true>), grid, dim3(64 * NW), s, a);
+        return;
+    }
+    DUO_LAUNCH((moe_down_kernel<W, MT, NB, NW, PF, false>), grid, dim3(64 * NW), s, a);
     duo_internal_prof(DUO_PROF_MOE_DOWN);
     DUO_LAUNCH(moe_combine_kernel, dim3((a.d + 1023) / 1024, a.rows), dim3(256), s, a);
 }
@@ -73,6 +78,12 @@ void launch_products(const MoeArgs& a, hipStream_t s) {
         launch_gate_up<W, 3, 4, 1>(a, s);
         launch_down<W, 3, 4, 4, 1>(a, s);
     }
+}
+
+int launch_experts(const duo_moe_config* cfg, const MoeArgs& a, hipStream_t s) {
+    if (cfg->scaled) launch_products<Narrow>(a, s);
+    else launch_products<Wide>(a, s);
+    return duo_internal_hip_ok(hipGetLastError(), "duo_moe_layer");
 }
 
 }  // namespace
@@ -133,10 +144,12 @@ extern "C" int duo_moe_layer(const duo_moe_config* cfg, const uint16_t* router, 
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // not of an earlier call
     duo_internal_prof(DUO_PROF_MOE_ROUTER);
+    if (router_in_one(a.n_experts, d)) {
+        DUO_LAUNCH(moe_router_kernel, dim3((rows + 15) / 16), dim3(64 * ROUTER_WAVES), s, a);
+        return launch_experts(cfg, a, s);
+    }
     DUO_LAUNCH(moe_logits_kernel, dim3(logit_parts(d), (a.n_experts + 15) / 16, (rows + 15) / 16), dim3(64 * LOGIT_WAVES), s, a);
     duo_internal_prof(DUO_PROF_MOE_ROUTER);
     DUO_LAUNCH(moe_choice_kernel, dim3(rows), dim3(CHOICE_THREADS), s, a);
-    if (cfg->scaled) launch_products<Narrow>(a, s);
-    else launch_products<Wide>(a, s);
-    return duo_internal_hip_ok(hipGetLastError(), "duo_moe_layer");
+    return launch_experts(cfg, a, s);
 }

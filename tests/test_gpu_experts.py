@@ -38,7 +38,8 @@ def check(layer, router, held, x, got, rows=None):
 
 # experts, d_model, d_ff, top_k, rows
 SHAPES = [(1, 64, 32, 1, 1), (4, 128, 96, 1, 3), (8, 64, 160, 2, 16), (5, 192, 128, 5, 17), (16, 256, 64, 4, 33), (3, 512, 416, 2, 47), (64, 128, 32, 6, 64),
-          (2, 320, 288, 1, 80), (512, 64, 32, 16, 80), (130, 64, 64, 8, 79), (8, 1024, 1408, 2, 9), (40, 64, 32, 3, 1), (4, 4096, 256, 2, 5), (6, 64, 4352, 2, 7)]
+          (2, 320, 288, 1, 80), (512, 64, 32, 16, 80), (130, 64, 64, 8, 79), (8, 1024, 1408, 2, 9), (40, 64, 32, 3, 1), (4, 4096, 256, 2, 5), (6, 64, 4352, 2, 7),
+          (32, 64, 64, 16, 17), (33, 128, 32, 16, 31), (17, 192, 32, 3, 33), (2, 64, 128, 1, 80), (3, 64, 96, 3, 80)]
 
 
 @BOTH
@@ -209,9 +210,11 @@ def test_a_mlp_and_a_head_held_in_8_bits(scaled, dtype):
     assert torch.equal(logits.argmax(1).cpu(), best)
 
 
+# experts, top_k -> launches of the router (one for small ones), of the down product (and the sum over a row's experts)
+@pytest.mark.parametrize("n,top_k,router_launches,down_launches", [(4, 2, 1, 2), (32, 1, 1, 1), (33, 2, 2, 2)])
 @BOTH
-def test_timer_sees_the_launches(dtype):
-    layer, _, _ = make(4, 64, 32, 2, dtype, False)
+def test_timer_sees_the_launches(dtype, n, top_k, router_launches, down_launches):
+    layer, _, _ = make(n, 64, 32, top_k, dtype, False)
     x = _randn((5, 64), dtype, 1)
     layer.run(x)
     torch.cuda.synchronize()
@@ -222,7 +225,7 @@ def test_timer_sees_the_launches(dtype):
         prof = B.profile_read(dtype)
     finally:
         B.profile_enable(False, dtype)
-    want = {"moe_router": 2, "moe_gate_up": 1, "moe_down": 2}  # logits and choice; product and sum over a row's experts
+    want = {"moe_router": router_launches, "moe_gate_up": 1, "moe_down": down_launches}
     assert all(p["launches"] == want.get(name, 0) for name, p in prof.items())
 
 
