@@ -266,25 +266,29 @@ __global__ __launch_bounds__(256) void scaled_rows_kernel(ScaledArgs a) {
 
 // then the product.  GB x GM waves, each WB bands x WM row tiles, on a block of features x rows.  Both operands lie in tiles as the matrix units take
 // them, so a stage (128 columns of the block) is a list of 1 KiB pieces that go from global memory straight into LDS, one lane's 16 bytes behind the
-// other's, and are read back the same way: no bank conflicts, no registers on the way.  Two stages: the next one is requested right behind the
-// barrier that says that everybody has left its place, and has all the products of this one to arrive.
-// 16-bit outputs use the 8-bit instruction, which applies the scales itself (a byte of a word for every row and block); fp32 outputs use the
-// 16-bit instruction on values that were converted with their scales, exactly, at half the rate.
-template <int WB, int WM, int GB, int GM, bool FP32>
+// other's, and are read back the same way: no bank conflicts, no registers on the way.  A stage is requested right behind the
+// barrier that says that everybody has left its place, STAGES - 1 steps before its products.
+// Products are 32 x 32: a lane takes row l % 32 of two tiles and, of each half of the 128 columns, pieces 2 (l / 32) and 2 (l / 32) + 1 of four.  16-bit
+// outputs use the 8-bit instruction, 32 x 32 x 64, which applies the scales itself (a byte of a word for every row and block; 4.0 PFLOP/s in a loop of
+// nothing else, 16 x 16 x 128 3.1 with one wave on a SIMD and 3.9 with two).  fp32 outputs use the 16-bit instruction on values that were converted
+// with their scales, exactly, at half the rate.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <int WB, int WM, int GB, int GM, int STAGES, bool FP32>
 __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a) {
     constexpr int WAVES = GB * GM, BB = WB * GB, BM = WM * GM;  // bands and row tiles of the block
     constexpr int PIECES = 2 * (BB + BM), EACH = PIECES / WAVES;
-    static_assert(PIECES % WAVES == 0 && WM == 4 && 8 % WB == 0, "equal loads for all; a wave's row tiles share a word of scales, its bands a scale");
-    __shared__ u32x4 lds[2][PIECES * 64];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    static_assert(PIECES % WAVES == 0 && WM == 4 && WB % 2 == 0 && 8 % WB == 0, "equal loads for all; a wave's row tiles share a word of scales, its bands a scale");
+    // a stage: the pieces, then for every wave 64 words: its rows' scales and, from word 16 on, the one with its bands' scale.  (One array: the compiler
+    // waits for loads on their way to an array of scales in front of every read of it.)
+    __shared__ u32x4 lds[STAGES][PIECES * 64 + WAVES * 16];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, half = lane >> 5, odd = lane >> 4 & 1;
     // Workgroups are dealt to the eight dies in turn.  Each die gets a run of neighbouring blocks: four blocks of rows by as many of features, so
     // that what a die reads at a time is shared by many of its workgroups.
     const int feature_blocks = (scaled_blocks(a.N) * 8 + BB - 1) / BB, row_blocks = (a.row_tiles + BM - 1) / BM, blocks = feature_blocks * row_blocks;
     const int share = (blocks + 7) / 8, id = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= share || id >= blocks) return;
-    const int band_of_four = id / (4 * feature_blocks), in_four = id - band_of_four * 4 * feature_blocks;
-    const int tall = min(4, row_blocks - band_of_four * 4);
-    const int rb = band_of_four * 4 + in_four % tall, fb = in_four / tall;
+    const int four = id / (4 * feature_blocks), in_four = id - four * 4 * feature_blocks, tall = min(4, row_blocks - four * 4);
+    const int rb = four * 4 + in_four % tall, fb = in_four / tall;
     const int band_last = scaled_blocks(a.N) * 8 - 1, tile_last = a.row_tiles - 1;
     const int wb = wave % GB, wm = wave / GB;
     const int band0 = fb * BB + wb * WB, tile0 = rb * BM + wm * WM;
@@ -296,77 +300,111 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
         const uint8_t* p = t < BB ? a.w + (size_t)min(fb * BB + t, band_last) * a.KB * SCALED_TILE : a.xq + (size_t)min(rb * BM + t - BB, tile_last) * a.KB * SCALED_TILE;
         from[i] = reinterpret_cast<const u32x4*>(p + (piece & 1) * 1024) + lane;
     }
-    const uint8_t* w_scale = a.w + a.w_scales + (size_t)(min(band0, band_last) >> 3) * a.KB;
-    const uint8_t* x_scale = a.xq + a.x_scales + row_scale_at(a.row_tiles, 0, min(tile0, tile_last) & ~3, c);
+    const size_t w_scale = a.w_scales + (size_t)(min(band0, band_last) >> 3) * a.KB;  // a byte for every stage, in words that are read whole
     const size_t x_step = row_scale_at(a.row_tiles, 1, 0, 0);
-    auto request = [&](int j) {
+    const uint8_t* const word = lane < 16 ? a.xq + a.x_scales + row_scale_at(a.row_tiles, 0, min(tile0, tile_last) & ~3, c) : a.w;
+    auto request = [&](int j, int slot) {  // beyond the end the last one again: as many loads as ever, for the wait below
+        j = min(j, a.KB - 1);
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[i] + (size_t)j * (SCALED_TILE / 16)),
-                                             (__attribute__((address_space(3))) void*)(&lds[j & 1][(wave * EACH + i) * 64]), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void*)(&lds[slot][(wave * EACH + i) * 64]), 16, 0, 0);
+        const size_t of_rows = (size_t)j * x_step, of_bands = (w_scale + j) & ~(size_t)3;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(word + (lane < 16 ? of_rows : of_bands)),
+                                         (__attribute__((address_space(3))) void*)(&lds[slot][PIECES * 64 + wave * 16]), 4, 0, 0);
     };
-    f32x4 acc[WB][WM];
+    // vmcnt: all but the youngest STAGES - 2 requests have landed (expcnt and lgkmcnt fields at their maxima)
+    constexpr int YOUNGER = (STAGES - 2) * (EACH + 1), WAIT = (YOUNGER & 15) | ((YOUNGER >> 4) << 14) | (7 << 4) | (15 << 8);
+    static_assert(YOUNGER <= 63, "the counter's range");
+    f32x16 acc[WB / 2][WM / 2];
 #pragma unroll
-    for (int b = 0; b < WB; ++b)
+    for (int b = 0; b < WB / 2; ++b)
 #pragma unroll
-        for (int m = 0; m < WM; ++m) acc[b][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-    request(0);
-    int sw_next = w_scale[0], sx_next = *reinterpret_cast<const int*>(x_scale);
+        for (int m = 0; m < WM / 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[b][m][i] = 0.f;
+#pragma unroll
+    for (int j = 0; j + 1 < STAGES; ++j) request(j, j);
+    int slot = 0;
     for (int j = 0; j < a.KB; ++j) {
-        const int sw = sw_next, sx = sx_next;
-        __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): this wave's pieces of stage j have landed
-        __builtin_amdgcn_s_barrier();                      // and everybody's; nobody reads stage j - 1 any more
-        if (j + 1 < a.KB) {
-            request(j + 1);
-            sw_next = w_scale[j + 1];
-            sx_next = *reinterpret_cast<const int*>(x_scale + (size_t)(j + 1) * x_step);
-        }
-        const u32x4* stage = &lds[j & 1][lane];
+        __builtin_amdgcn_s_waitcnt(WAIT);  // this wave's pieces of stage j have landed
+        __builtin_amdgcn_s_barrier();      // and everybody's; nobody reads stage j - 1 any more
+        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(&lds[slot][PIECES * 64 + wave * 16]);
+        const int sx = (int)(scales[c] >> (8 * odd));  // byte 0: the lane's row of the first two row tiles, byte 2: of the others
+        const int sw = (int)(scales[16] >> (8 * ((w_scale + j) & 3)) & 255u);
+        const u32x4* stage = &lds[slot][odd * 128 + half * 32 + c];
         const u32x4 *ws = stage + wb * WB * 128, *xs = stage + (BB + wm * WM) * 128;
-        if constexpr (FP32) {
-            const float fw = scale_of(sw);
-            float fx[4];
+        auto operand = [](const u32x4* t) {
+            const u32x4 p = t[0], q = t[16];
+            return i32x8{(int)p[0], (int)p[1], (int)p[2], (int)p[3], (int)q[0], (int)q[1], (int)q[2], (int)q[3]};
+        };
+        // what the first products need is on its way out of LDS while the requests go out
+        i32x8 x[2][WM / 2], next = operand(ws);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) fx[m] = scale_of(sx >> (8 * m) & 255);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 x[WM];
+            for (int m = 0; m < WM / 2; ++m) x[h][m] = operand(xs + m * 256 + h * 64);
+        __builtin_amdgcn_sched_barrier(0);
+        request(j + STAGES - 1, slot == 0 ? STAGES - 1 : slot - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
 #pragma unroll
-                for (int m = 0; m < WM; ++m) x[m] = xs[m * 128 + h * 64];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    bf16x8 u[WM];
+            for (int b = 0; b < WB / 2; ++b) {  // two bands' tiles are read while the products of the two before run
+                const i32x8 w = next;
+                const int t = h * (WB / 2) + b + 1;
+                if (t < WB) next = operand(ws + t % (WB / 2) * 256 + t / (WB / 2) * 64);
+                if constexpr (FP32) {
+                    const float fw = scale_of(sw), fx[2] = {scale_of(sx & 255), scale_of(sx >> 16 & 255)};
 #pragma unroll
-                    for (int m = 0; m < WM; ++m) u[m] = e4m3_to_bf16(x[m][2 * i], x[m][2 * i + 1], fx[m]);
+                    for (int i = 0; i < 4; ++i) {
+                        const bf16x8 f = e4m3_to_bf16(w[2 * i], w[2 * i + 1], fw);
 #pragma unroll
-                    for (int b = 0; b < WB; ++b) {
-                        const u32x4 w = ws[b * 128 + h * 64];
-                        const bf16x8 v = e4m3_to_bf16(w[2 * i], w[2 * i + 1], fw);
-#pragma unroll
-                        for (int m = 0; m < WM; ++m) acc[b][m] = mfma_bf16(v, u[m], acc[b][m]);
+                        for (int m = 0; m < WM / 2; ++m)
+                            acc[b][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, e4m3_to_bf16(x[h][m][2 * i], x[h][m][2 * i + 1], fx[m]), acc[b][m], 0, 0, 0);
                     }
+                } else {
+                    acc[b][0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x[h][0], acc[b][0], 0, 0, 0, sw, 0, sx);
+                    acc[b][1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x[h][1], acc[b][1], 0, 0, 0, sw, 2, sx);
                 }
             }
-        } else {
-            auto whole = [](const u32x4* t) {
-                const u32x4 p = t[0], q = t[64];
-                return i32x8{(int)p[0], (int)p[1], (int)p[2], (int)p[3], (int)q[0], (int)q[1], (int)q[2], (int)q[3]};
-            };
-            i32x8 x[WM];
+    }
+    // Outputs, 32 rows at a time, through a wave's own piece of LDS, so that a store covers 128 to 256 bytes of a row instead of 16.  Register i of a
+    // lane: feature 8 (i / 4) + 4 half + i % 4 of two bands, row l % 32.
+    constexpr int BYTES = FP32 ? 4 : 2, ROW = WB * 16 * BYTES, PITCH = ROW + 16, CHUNKS = ROW / 16, ROWS = 64 / CHUNKS;  // ROWS in one store
+    static_assert(sizeof(lds) >= (size_t)WAVES * 32 * PITCH, "32 rows of every wave");
+    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): nothing is on its way to LDS any more,
+    __builtin_amdgcn_s_barrier();                      // and nobody reads a stage (every wave's reads have gone into products)
+    char* const mine = reinterpret_cast<char*>(&lds[0][0]) + wave * 32 * PITCH;
+    const int n = band0 * 16 + lane % CHUNKS * (16 / BYTES);
 #pragma unroll
-            for (int m = 0; m < WM; ++m) x[m] = whole(xs + m * 128);
+    for (int m = 0; m < WM / 2; ++m) {
 #pragma unroll
-            for (int b = 0; b < WB; ++b) {
-                const i32x8 w = whole(ws + b * 128);
-                acc[b][0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[0], acc[b][0], 0, 0, 0, sw, 0, sx);
-                acc[b][1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[1], acc[b][1], 0, 0, 0, sw, 1, sx);
-                acc[b][2] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[2], acc[b][2], 0, 0, 0, sw, 2, sx);
-                acc[b][3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x[3], acc[b][3], 0, 0, 0, sw, 3, sx);
+        for (int b = 0; b < WB / 2; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                char* at = mine + (lane & 31) * PITCH + (b * 32 + 8 * q + 4 * half) * BYTES;
+                const f32x4 v = {acc[b][m][4 * q], acc[b][m][4 * q + 1], acc[b][m][4 * q + 2], acc[b][m][4 * q + 3]};
+                if constexpr (FP32) *reinterpret_cast<f32x4*>(at) = v;
+                else *reinterpret_cast<uint2*>(at) = make_uint2(pack_elem2(v[0], v[1]), pack_elem2(v[2], v[3]));
+            }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) {
+            const int r = i * ROWS + lane / CHUNKS, row = (tile0 + 2 * m) * 16 + r;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * PITCH + lane % CHUNKS * 16);
+            if (row < a.rows && n < a.N) {
+                char* y = static_cast<char*>(a.y) + ((size_t)row * a.y_stride + n) * BYTES;
+                if (n + 16 / BYTES <= a.N) *reinterpret_cast<u32x4*>(y) = v;
+                else if constexpr (FP32)
+                    for (int k = 0; k < a.N - n; ++k) reinterpret_cast<uint32_t*>(y)[k] = v[k];
+                else
+                    for (int k = 0; k < a.N - n; ++k) reinterpret_cast<u16*>(y)[k] = (u16)((k < 4 ? k < 2 ? v[0] : v[1] : k < 6 ? v[2] : v[3]) >> (16 * (k & 1)));
             }
         }
+        __builtin_amdgcn_wave_barrier();  // LDS serves a wave's accesses in order: the next rows' writes follow these reads
     }
-#pragma unroll
-    for (int b = 0; b < WB; ++b)
-#pragma unroll
-        for (int m = 0; m < WM; ++m) store_outputs<FP32>(a, (tile0 + m) * 16 + c, (band0 + b) * 16 + 4 * g, acc[b][m]);
 }

@@ -32,11 +32,11 @@ void launch_stream(const ScaledArgs& a, hipStream_t s) {
     else launch_bands<MT, 4, 2, 2, FP32>(a, s);
 }
 int blocks_of(const ScaledArgs& a, int bands, int tiles) { return (scaled_blocks(a.N) * 8 + bands - 1) / bands * ((a.row_tiles + tiles - 1) / tiles); }
-template <int WB, int WM, int GB, int GM, bool FP32>
+template <int WB, int WM, int GB, int GM, int STAGES, bool FP32>
 void launch_block(const ScaledArgs& a, hipStream_t s) {
     const int blocks = blocks_of(a, WB * GB, WM * GM);
     duo_internal_prof(DUO_PROF_SCALED);
-    DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, FP32>), dim3((blocks + 7) / 8 * 8), dim3(64 * GB * GM), s, a);
+    DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, STAGES, FP32>), dim3((blocks + 7) / 8 * 8), dim3(64 * GB * GM), s, a);
 }
 
 template <bool FP32>
@@ -52,14 +52,31 @@ void launch_product(const ScaledArgs& a, hipStream_t s) {
         case 4: return launch_stream<4, FP32>(a, s);
         case 5: return launch_stream<5, FP32>(a, s);
     }
-    // Blocks of 256 x 256, one to a compute unit, or of 128 x 128, two to one: two of the small ones take 0.54 of the time of a large one (8192^3: 452
-    // us against 484), so what decides is how the last round comes out (999 rows, 5120 x 13824: 159 us in large blocks, 87 in small ones).
-    // In fp32 the large one has no registers left.
-    if constexpr (!FP32) {
-        const int large = (blocks_of(a, 16, 16) + 255) / 256, small = (blocks_of(a, 8, 8) + 511) / 512;
-        if (large * 100 <= small * 54) return launch_block<8, 4, 2, 4, FP32>(a, s);
+    // The block that is through first: rounds of the chip times what a step of 128 columns takes with a workgroup (of the 128 x 128 of four waves: two)
+    // on every compute unit.  The steps were measured on 8192^3 and, the two small blocks, on 300 and 100 rows of 4096 x 4096, where a step is
+    // mostly waiting and one workgroup a unit all there is.  16-bit outputs: 999 rows, 12288 x 4096: 256 x 256 52 us, 128 x 256 67, 128 x 128 69;
+    // 5120 x 13824: 173, 101, 108; 300 rows, 4096 x 4096: 64 x 128 17 us, 128 x 128 24; 100 rows: 64 x 64 14 us, 64 x 128 17.
+    struct Block {
+        int bands, tiles, a_unit;
+        double narrow, wide;  // us a step; wide: fp32 outputs (256 x 256 has no LDS for them)
+    };
+    constexpr Block blocks[] = {{16, 16, 1, 1.70, 1e9}, {8, 16, 1, 1.03, 1.85}, {8, 8, 2, 1.05, 1.80}, {8, 8, 1, 0.60, 1.10}, {4, 8, 1, 0.42, 0.60}, {4, 4, 1, 0.35, 0.59}};
+    int best = 0;
+    double least = 1e18;
+    for (int i = 0; i < 6; ++i) {
+        const int at_once = 256 * blocks[i].a_unit;
+        const double t = ((blocks_of(a, blocks[i].bands, blocks[i].tiles) + at_once - 1) / at_once) * (FP32 ? blocks[i].wide : blocks[i].narrow);
+        if (t < least) least = t, best = i;
     }
-    launch_block<4, 4, 2, 2, FP32>(a, s);
+    if constexpr (!FP32)
+        if (best == 0) return launch_block<8, 4, 2, 4, 2, FP32>(a, s);
+    switch (best) {
+        case 1: return launch_block<4, 4, 2, 4, 3, FP32>(a, s);
+        case 2: return launch_block<4, 4, 2, 2, 2, FP32>(a, s);
+        case 3: return launch_block<2, 4, 4, 2, 4, FP32>(a, s);
+        case 4: return launch_block<2, 4, 2, 2, 3, FP32>(a, s);
+        default: return launch_block<2, 4, 2, 1, 4, FP32>(a, s);
+    }
 }
 
 }  // namespace

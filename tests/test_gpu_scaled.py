@@ -55,7 +55,8 @@ def test_rows_times_the_identity_are_the_rows_in_8_bits(rows, fp32, dtype):
 
 SHAPES = [(1, 64, 128), (1, 4096, 4096), (2, 17, 32), (5, 1, 96), (8, 130, 1056), (15, 515, 416), (16, 256, 2048), (17, 100, 352), (33, 1031, 1408), (48, 48, 5120),
           (49, 300, 160), (64, 4099, 512), (79, 128, 11008), (80, 640, 608), (81, 640, 608), (100, 33, 96), (128, 128, 128), (129, 1000, 1408), (257, 515, 4096),
-          (600, 4099, 288), (1023, 2050, 1056)]
+          (600, 4099, 288), (1023, 2050, 1056),
+          (100, 9000, 160), (500, 4096, 416), (999, 12290, 160), (2000, 4096, 288), (999, 5120, 416), (1500, 8200, 96), (90, 200, 4096), (128, 40000, 96)]
 
 
 @BOTH
