@@ -724,11 +724,12 @@ class _OnDevice:
             raise ValueError(f"{name} must be {types[0]} [rows][{width}] on {self.device}, not {t.dtype} {list(shape)} on {t.device}")
         if stride[1] != 1 and width > 1:
             raise ValueError(f"{name}: the elements of a row must lie together")
-        each = 16 // t.element_size()
-        distance = stride[0] if shape[0] > 1 else (width + each - 1) // each * each
-        if shape[0] > 1 and distance < width:
+        rows, distance = shape[0], stride[0]
+        if rows <= 1:
+            distance = (width + 7) // 8 * 8  # no other row: whatever torch says, it is not used
+        elif distance < width:
             raise ValueError(f"{name}: rows overlap" if writes else f"{name}: rows must lie one behind the other")
-        return t.data_ptr(), shape[0], distance
+        return t.data_ptr(), rows, distance
 
 
 def _type_name(w) -> str:

@@ -87,16 +87,20 @@ struct ReadyPiece {
     u32x4 v[2];
     int byte;
     struct Source {
-        const u32x4* tile;
-        const uint8_t* scale;
+        __amdgpu_buffer_rsrc_t rows;  // lanes behind the last row ask for what lies behind the end and get zeros without a memory access
+        uint32_t tile, scale;
     };
     static __device__ __forceinline__ Source source(const ScaledArgs& a, int tile, int lane) {
-        return {reinterpret_cast<const u32x4*>(a.xq + (size_t)tile * a.KB * SCALED_TILE) + lane, a.xq + a.x_scales + row_scale_at(a.row_tiles, 0, tile, lane & 15)};
+        const int c = lane & 15;
+        const uint32_t none = tile * 16 + c < a.rows ? 0u : 0x80000000u;
+        const size_t bytes = a.x_scales + row_scale_bytes(a.row_tiles, a.KB);  // at most 5 tiles of 512 blocks: 5.5 MB
+        return {__builtin_amdgcn_make_buffer_rsrc(a.xq, 0, (uint32_t)bytes, 0x00027000), none + (uint32_t)tile * a.KB * SCALED_TILE + lane * 16,
+                none + (uint32_t)(a.x_scales + row_scale_at(a.row_tiles, 0, tile, c))};
     }
     __device__ __forceinline__ void load(Source s, int j, const ScaledArgs& a, int) {
-        v[0] = s.tile[(size_t)j * (SCALED_TILE / 16)];
-        v[1] = s.tile[(size_t)j * (SCALED_TILE / 16) + 64];
-        byte = s.scale[row_scale_at(a.row_tiles, j, 0, 0)];
+        v[0] = __builtin_amdgcn_raw_buffer_load_b128(s.rows, (int)(s.tile + (uint32_t)j * SCALED_TILE), 0, 0);
+        v[1] = __builtin_amdgcn_raw_buffer_load_b128(s.rows, (int)(s.tile + (uint32_t)j * SCALED_TILE + 1024), 0, 0);
+        byte = __builtin_amdgcn_raw_buffer_load_b8(s.rows, (int)(s.scale + (uint32_t)row_scale_at(a.row_tiles, j, 0, 0)), 0, 0);
     }
     __device__ __forceinline__ float e4m3(int, int, int, u32x4 (&q)[2]) {
         q[0] = v[0], q[1] = v[1];

@@ -21,16 +21,23 @@ void launch_bands(const ScaledArgs& a, hipStream_t s) {
     duo_internal_prof(DUO_PROF_SCALED);
     DUO_LAUNCH((scaled_stream_kernel<MT, NB, NW, PF, (MT > DUO_SCALED_DIRECT_ROWS / 16), FP32>), dim3((bands + NB - 1) / NB), dim3(64 * NW), s, a);
 }
+// Bands a workgroup, waves, blocks of columns a wave has on their way.  Few bands: one or two a workgroup, so that there is one workgroup for every
+// compute unit; up to 1024 bands four, all workgroups at once in one round; beyond, what leaves the rounds even.  us for 9 rows, 4096 columns:
+// 256 bands 5.9 (one band, eight waves; two bands 7.1), 768 bands 10.5 (four; two 11.4), 1376 bands 17.0 (two; four 18.5), 8016 bands 80 (two or four).
+// Rows that were brought to e4m3 beforehand, 33 of them: 256 bands 9.7, 768 15.7, 1376 23.9 (four bands 24.9), 8016 90 (four bands and one wave; two
+// waves 98), each with the 3 us of the launch in front.
 template <int MT, bool FP32>
 void launch_stream(const ScaledArgs& a, hipStream_t s) {
     const int bands = (a.N + 15) / 16;
     if (bands <= 256) launch_bands<MT, 1, 8, (MT == 2 ? 1 : 2), FP32>(a, s);
     else if (bands <= 512) launch_bands<MT, 2, 8, (MT == 2 ? 1 : 2), FP32>(a, s);
-    else if (bands <= 1024) launch_bands<MT, 4, (MT == 2 ? 4 : 8), (MT == 2 ? 2 : 1), FP32>(a, s);
+    else if (bands <= 1024) launch_bands<MT, 4, (MT == 1 ? 8 : 4), (MT == 1 ? 1 : 2), FP32>(a, s);
     else if constexpr (MT == 1) launch_bands<MT, 2, 8, 2, FP32>(a, s);
     else if constexpr (MT == 2) launch_bands<MT, 4, 4, 1, FP32>(a, s);
-    else launch_bands<MT, 4, 2, 2, FP32>(a, s);
+    else if (bands <= 4096) launch_bands<MT, 4, 2, 2, FP32>(a, s);
+    else launch_bands<MT, 4, 1, 2, FP32>(a, s);
 }
+
 int blocks_of(const ScaledArgs& a, int bands, int tiles) { return (scaled_blocks(a.N) * 8 + bands - 1) / bands * ((a.row_tiles + tiles - 1) / tiles); }
 template <int WB, int WM, int GB, int GM, int STAGES, bool FP32>
 void launch_block(const ScaledArgs& a, hipStream_t s) {
@@ -39,6 +46,8 @@ void launch_block(const ScaledArgs& a, hipStream_t s) {
     DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, STAGES, FP32>), dim3((blocks + 7) / 8 * 8), dim3(64 * GB * GM), s, a);
 }
 
+// Up to DUO_SCALED_DIRECT_ROWS rows every workgroup brings them to e4m3 for itself.  Beyond, that costs more than a launch that does it once (33 rows of
+// 22016 x 4096: 29.8 us, 23.9 with the launch; 17 rows of 4096 x 4096: 8.6, 9.0).
 template <bool FP32>
 void launch_product(const ScaledArgs& a, hipStream_t s) {
     if (a.rows > DUO_SCALED_DIRECT_ROWS) {
