@@ -423,7 +423,7 @@ int duo_page_commit(const duo_model_config *cfg, const duo_page_cache *cache, co
 #define DUO_SCALED_MAX_N      1048576
 #define DUO_SCALED_MAX_K      65536
 #define DUO_SCALED_MAX_ROWS   262144
-#define DUO_SCALED_DIRECT_ROWS 32  /* up to which a product needs no workspace */
+#define DUO_SCALED_DIRECT_ROWS 16  /* up to which a product needs no workspace */
 #define DUO_SCALED_MAX_STRIDE 2147483647 /* elements from row to row */
 size_t duo_scaled_bytes(int N, int K);
 int duo_scaled_pack(const uint16_t *src, int N, int K, void *dst, void *hip_stream);

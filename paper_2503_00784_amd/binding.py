@@ -27,7 +27,7 @@ PAGE_NO_PAGES, PAGE_BAD_REQUEST, PAGE_BAD_PAGE, PAGE_NO_PLAN, PAGE_BAD_RECORD = 
 PAGE_MAX_REQUESTS = 4096
 PAGE_MAX_ROWS = 262144
 PAGE_MAX_SLOTS = 8388608
-SCALED_MAX_N, SCALED_MAX_K, SCALED_MAX_ROWS, SCALED_DIRECT_ROWS = 1048576, 65536, 262144, 32
+SCALED_MAX_N, SCALED_MAX_K, SCALED_MAX_ROWS, SCALED_DIRECT_ROWS = 1048576, 65536, 262144, 16
 MOE_MAX_EXPERTS, MOE_MAX_TOP = 512, 16
 
 EXPORTS = ["duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample_workspace_bytes",
@@ -794,8 +794,9 @@ class ScaledMatrix(_OnDevice):
             need = C.c_size_t(0)
             _check(self.lib.duo_scaled_workspace_bytes(rows, self.N, self.K, C.byref(need)), "duo_scaled_workspace_bytes")
             nbytes = need.value
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)  # of this call and its stream
-            wp = workspace.data_ptr()
+            if nbytes:
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)  # of this call and its stream
+                wp = workspace.data_ptr()
         self._call(self._gemm, xp, xs, self._ptr, yp, ys, 1 if out.dtype == torch.float32 else 0, rows, self.N, self.K, wp, nbytes)
         return out
 

@@ -67,10 +67,11 @@ void launch_products(const MoeArgs& a, hipStream_t s) {
     const int each = a.rows * a.top / a.n_experts;
     if (each <= 12 || a.rows <= 16) {
         launch_gate_up<W, 1, 4, 2>(a, s);
-        // four bands for two waves where that makes enough workgroups (128 experts of 4096 x 1536 in 8 bits: 145 us, two bands for four waves 171; two
-        // experts of 4096 x 14336: 30, 22)
+        // four bands for two waves where that makes enough workgroups (128 experts of 4096 x 1536 in 8 bits: 145 us, two bands for four waves 171), two
+        // for four where not (two experts of 4096 x 14336: 22, four bands 30), and one for eight where the outputs are few (two experts of 320 x 7680: 9.4, two bands 14.7)
         if (most_active(a) * a.d > 16384) launch_down<W, 1, 4, 2, 1>(a, s);
-        else launch_down<W, 1, 2, 4, 2>(a, s);
+        else if (most_active(a) * a.d > 4096) launch_down<W, 1, 2, 4, 2>(a, s);
+        else launch_down<W, 1, 1, 8, 1>(a, s);
     } else if (each <= 28) {
         launch_gate_up<W, 2, 4, 1>(a, s);
         launch_down<W, 2, 4, 4, 1>(a, s);

@@ -10,32 +10,45 @@ bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; 
 
 int check_matrix(int N, int K) { return N < 1 || N > DUO_SCALED_MAX_N || K < 32 || K % 32 || K > DUO_SCALED_MAX_K ? DUO_ERR_SHAPE : DUO_OK; }
 
+// Whether a launch of its own brings the rows to e4m3 before the product; if not, every workgroup does it for itself, which for more than 16 rows
+// costs more than the launch unless there are few columns: 26 rows of 96 x 14784 25 us, 16 with the launch; 17 of 22016 x 4096 22.2, 20.0; 17 of 8192 x
+// 1024 4.6, 6.8.
+bool rows_first(int rows, int K) { return rows > DUO_SCALED_DIRECT_ROWS && !(rows <= 32 && K <= 2048); }
 size_t rows_bytes(int rows, int K) {  // of the workspace: tiles and scales of the rows
     const int tiles = (rows + 15) / 16, blocks = scaled_blocks(K);
-    return rows <= DUO_SCALED_DIRECT_ROWS ? 0 : (size_t)tiles * blocks * SCALED_TILE + row_scale_bytes(tiles, blocks);
+    return rows_first(rows, K) ? (size_t)tiles * blocks * SCALED_TILE + row_scale_bytes(tiles, blocks) : 0;
 }
 
-template <int MT, int NB, int NW, int PF, bool FP32>
+template <int MT, int NB, int NW, int PF, bool READY, bool FP32>
 void launch_bands(const ScaledArgs& a, hipStream_t s) {
     const int bands = (a.N + 15) / 16;
     duo_internal_prof(DUO_PROF_SCALED);
-    DUO_LAUNCH((scaled_stream_kernel<MT, NB, NW, PF, (MT > DUO_SCALED_DIRECT_ROWS / 16), FP32>), dim3((bands + NB - 1) / NB), dim3(64 * NW), s, a);
+    DUO_LAUNCH((scaled_stream_kernel<MT, NB, NW, PF, READY, FP32>), dim3((bands + NB - 1) / NB), dim3(64 * NW), s, a);
 }
 // Bands a workgroup, waves, blocks of columns a wave has on their way.  Few bands: one or two a workgroup, so that there is one workgroup for every
 // compute unit; up to 1024 bands four, all workgroups at once in one round; beyond, what leaves the rounds even.  us for 9 rows, 4096 columns:
 // 256 bands 5.9 (one band, eight waves; two bands 7.1), 768 bands 10.5 (four; two 11.4), 1376 bands 17.0 (two; four 18.5), 8016 bands 80 (two or four).
-// Rows that were brought to e4m3 beforehand, 33 of them: 256 bands 9.7, 768 15.7, 1376 23.9 (four bands 24.9), 8016 90 (four bands and one wave; two
-// waves 98), each with the 3 us of the launch in front.
 template <int MT, bool FP32>
-void launch_stream(const ScaledArgs& a, hipStream_t s) {
+void launch_direct(const ScaledArgs& a, hipStream_t s) {
     const int bands = (a.N + 15) / 16;
-    if (bands <= 256) launch_bands<MT, 1, 8, (MT == 2 ? 1 : 2), FP32>(a, s);
-    else if (bands <= 512) launch_bands<MT, 2, 8, (MT == 2 ? 1 : 2), FP32>(a, s);
-    else if (bands <= 1024) launch_bands<MT, 4, (MT == 1 ? 8 : 4), (MT == 1 ? 1 : 2), FP32>(a, s);
-    else if constexpr (MT == 1) launch_bands<MT, 2, 8, 2, FP32>(a, s);
-    else if constexpr (MT == 2) launch_bands<MT, 4, 4, 1, FP32>(a, s);
-    else if (bands <= 4096) launch_bands<MT, 4, 2, 2, FP32>(a, s);
-    else launch_bands<MT, 4, 1, 2, FP32>(a, s);
+    if (bands <= 256) launch_bands<MT, 1, 8, (MT == 1 ? 2 : 1), false, FP32>(a, s);
+    else if (bands <= 512) launch_bands<MT, 2, 8, (MT == 1 ? 2 : 1), false, FP32>(a, s);
+    else if (bands <= 1024) launch_bands<MT, 4, (MT == 1 ? 8 : 4), (MT == 1 ? 1 : 2), false, FP32>(a, s);
+    else if constexpr (MT == 1) launch_bands<MT, 2, 8, 2, false, FP32>(a, s);
+    else launch_bands<MT, 4, 4, 1, false, FP32>(a, s);
+}
+// The same where the rows are ready.  us for 33 rows, 4096 columns, with the 3 us of the launch in front: 256 bands 9.7 (one band, eight waves), 768 15.7
+// (four bands; two 17.3), 1376 23.9 (two; four 24.9), 8016 91 (four bands and one wave; two bands 110); two tiles of rows 8.2, 13.9, 20.2 and 84 (four bands and four waves).
+template <int MT, bool FP32>
+void launch_ready(const ScaledArgs& a, hipStream_t s) {
+    const int bands = (a.N + 15) / 16;
+    if (bands <= 256) launch_bands<MT, 1, 8, 2, true, FP32>(a, s);
+    else if (bands <= 512) launch_bands<MT, 2, 8, 2, true, FP32>(a, s);
+    else if (bands <= 1024) launch_bands<MT, 4, 4, 2, true, FP32>(a, s);
+    else if (bands <= 1536 || (MT == 2 && bands <= 4096)) launch_bands<MT, 2, 4, 2, true, FP32>(a, s);
+    else if constexpr (MT == 2) launch_bands<MT, 4, 4, 2, true, FP32>(a, s);
+    else if (bands <= 4096) launch_bands<MT, 4, 2, 2, true, FP32>(a, s);
+    else launch_bands<MT, 4, 1, 2, true, FP32>(a, s);
 }
 
 int blocks_of(const ScaledArgs& a, int bands, int tiles) { return (scaled_blocks(a.N) * 8 + bands - 1) / bands * ((a.row_tiles + tiles - 1) / tiles); }
@@ -46,21 +59,17 @@ void launch_block(const ScaledArgs& a, hipStream_t s) {
     DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, STAGES, FP32>), dim3((blocks + 7) / 8 * 8), dim3(64 * GB * GM), s, a);
 }
 
-// Up to DUO_SCALED_DIRECT_ROWS rows every workgroup brings them to e4m3 for itself.  Beyond, that costs more than a launch that does it once (33 rows of
-// 22016 x 4096: 29.8 us, 23.9 with the launch; 17 rows of 4096 x 4096: 8.6, 9.0).
 template <bool FP32>
 void launch_product(const ScaledArgs& a, hipStream_t s) {
-    if (a.rows > DUO_SCALED_DIRECT_ROWS) {
-        duo_internal_prof(DUO_PROF_SCALED);
-        DUO_LAUNCH(scaled_rows_kernel, dim3(a.KB, (a.row_tiles + 3) / 4), dim3(256), s, a);
-    }
-    switch (a.rows <= DUO_MAX_ROWS ? a.row_tiles : 0) {
-        case 1: return launch_stream<1, FP32>(a, s);
-        case 2: return launch_stream<2, FP32>(a, s);
-        case 3: return launch_stream<3, FP32>(a, s);
-        case 4: return launch_stream<4, FP32>(a, s);
-        case 5: return launch_stream<5, FP32>(a, s);
-    }
+    if (!rows_first(a.rows, a.K)) return a.row_tiles == 1 ? launch_direct<1, FP32>(a, s) : launch_direct<2, FP32>(a, s);
+    duo_internal_prof(DUO_PROF_SCALED);
+    DUO_LAUNCH(scaled_rows_kernel, dim3(a.KB, (a.row_tiles + 3) / 4), dim3(256), s, a);
+    if (a.rows <= DUO_MAX_ROWS) switch (a.row_tiles) {
+            case 2: return launch_ready<2, FP32>(a, s);
+            case 3: return launch_ready<3, FP32>(a, s);
+            case 4: return launch_ready<4, FP32>(a, s);
+            default: return launch_ready<5, FP32>(a, s);
+        }
     // The block that is through first: rounds of the chip times what a step of 128 columns takes with a workgroup (of the 128 x 128 of four waves: two)
     // on every compute unit.  The steps were measured on 8192^3 and, the two small blocks, on 300 and 100 rows of 4096 x 4096, where a step is
     // mostly waiting and one workgroup a unit all there is.  16-bit outputs: 999 rows, 12288 x 4096: 256 x 256 52 us, 128 x 256 67, 128 x 128 69;

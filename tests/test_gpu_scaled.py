@@ -56,7 +56,8 @@ def test_rows_times_the_identity_are_the_rows_in_8_bits(rows, fp32, dtype):
 SHAPES = [(1, 64, 128), (1, 4096, 4096), (2, 17, 32), (5, 1, 96), (8, 130, 1056), (15, 515, 416), (16, 256, 2048), (17, 100, 352), (33, 1031, 1408), (48, 48, 5120),
           (49, 300, 160), (64, 4099, 512), (79, 128, 11008), (80, 640, 608), (81, 640, 608), (100, 33, 96), (128, 128, 128), (129, 1000, 1408), (257, 515, 4096),
           (600, 4099, 288), (1023, 2050, 1056),
-          (100, 9000, 160), (500, 4096, 416), (999, 12290, 160), (2000, 4096, 288), (999, 5120, 416), (1500, 8200, 96), (90, 200, 4096), (128, 40000, 96)]
+          (100, 9000, 160), (500, 4096, 416), (999, 12290, 160), (2000, 4096, 288), (999, 5120, 416), (1500, 8200, 96), (90, 200, 4096), (128, 40000, 96),
+          (26, 96, 14784), (17, 4096, 4096), (30, 9000, 2080), (32, 20000, 96), (18, 70000, 32), (25, 8000, 2112), (40, 70000, 32), (66, 20000, 64), (50, 25000, 64)]
 
 
 @BOTH
@@ -164,7 +165,7 @@ def test_two_streams_at_once(rows):
 @BOTH
 def test_timer_sees_the_launches(dtype):
     m = B.ScaledMatrix(_randn((100, 256), dtype, 2))
-    few, many = _randn((32, 256), dtype, 1), _randn((90, 256), dtype, 1)
+    few, many = _randn((16, 256), dtype, 1), _randn((90, 256), dtype, 1)
     m.product(few), m.product(many)
     torch.cuda.synchronize()
     B.profile_enable(True, dtype)

@@ -37,7 +37,8 @@ def test_workspace_of_a_product(lib):
     assert f(1, 16, 32, None) == -1
     assert f(0, 16, 32, C.byref(out)) == f(B.SCALED_MAX_ROWS + 1, 16, 32, C.byref(out)) == f(1, 16, 33, C.byref(out)) == f(1, 0, 32, C.byref(out)) == -2
     assert out.value == 7
-    assert f(32, 4096, 4096, C.byref(out)) == 0 and out.value == 0
+    assert f(16, 4096, 4096, C.byref(out)) == 0 and out.value == 0
+    assert f(17, 4096, 4096, C.byref(out)) == 0 and out.value >= 17 * 4096
     assert f(33, 4096, 4096, C.byref(out)) == 0 and out.value >= 33 * 4096
     assert f(81, 4096, 4096, C.byref(out)) == 0 and out.value >= 81 * 4096
 
