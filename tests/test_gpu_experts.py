@@ -58,10 +58,10 @@ def test_layers(n, d, ff, top_k, rows, scaled, dtype):
 
 @BOTH
 @FORMS
-@pytest.mark.parametrize("rows", [15, 16, 33, 80])
-def test_every_row_on_the_same_experts(rows, scaled, dtype):
-    """One expert has all the rows, and experts have none."""
-    layer, router, held = make(6, 128, 96, 2, dtype, scaled)
+@pytest.mark.parametrize("n,rows", [(6, 15), (6, 16), (6, 33), (6, 80), (100, 17), (100, 49), (200, 80)])
+def test_every_row_on_the_same_experts(n, rows, scaled, dtype):
+    """One expert has all the rows, and experts have none; with fewer choices than experts and with more."""
+    layer, router, held = make(n, 128, 96, 2, dtype, scaled)
     x = _randn((rows, 128), dtype, 3, 0.01) + _randn((1, 128), dtype, 4)
     got = layer.run(x)
     check(layer, router, held, x, got)
@@ -70,8 +70,9 @@ def test_every_row_on_the_same_experts(rows, scaled, dtype):
 
 @BOTH
 @FORMS
-def test_rows_that_are_left_out(scaled, dtype):
-    layer, router, held = make(8, 128, 160, 2, dtype, scaled)
+@pytest.mark.parametrize("n", [8, 33, 90])
+def test_rows_that_are_left_out(n, scaled, dtype):
+    layer, router, held = make(n, 128, 160, 2, dtype, scaled)
     rows = 40
     x = _randn((rows, 128), dtype, 3)
     position = torch.arange(rows, dtype=torch.int32, device=DEV)
@@ -82,6 +83,9 @@ def test_rows_that_are_left_out(scaled, dtype):
     y = torch.full_like(x, 7.0)
     chosen, share = torch.full((rows, 2), 9, dtype=torch.int32, device=DEV), torch.full((rows, 2), 3.0, device=DEV)
     got = layer.run(x, y, position=position, chosen=chosen, share=share)
+    one = B.ExpertLayer(router, [tuple(w.to(x.dtype).to(DEV) for w in e) for e in held], 1, scaled=scaled)  # one choice a row: another way out
+    y1 = one.run(x, torch.full_like(x, 7.0), position=position)[0]
+    assert bool((y1[out_rows] == 7).all()) and bool(torch.isfinite(y1[keep]).all()) and not bool((y1[keep] == 7).all(1).any())
     clean = x.clone()
     clean[out_rows] = 0.0
     check(layer, router, held, clean, got, keep)
