@@ -282,8 +282,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int WB, int WM, int GB, int GM, int STAGES, bool FP32>
 __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a) {
     constexpr int WAVES = GB * GM, BB = WB * GB, BM = WM * GM;  // bands and row tiles of the block
-    constexpr int PIECES = 2 * (BB + BM), EACH = PIECES / WAVES;
-    static_assert(PIECES % WAVES == 0 && WM == 4 && WB % 2 == 0 && 8 % WB == 0, "equal loads for all; a wave's row tiles share a word of scales, its bands a scale");
+    constexpr int EACH = (2 * (BB + BM) + WAVES - 1) / WAVES, PIECES = EACH * WAVES;  // the last ones may be the last tile again, for nothing
+    static_assert(WM == 4 && WB % 2 == 0 && 8 % WB == 0, "a wave's row tiles share a word of scales, its bands a scale");
     // a stage: the pieces, then for every wave 64 words: its rows' scales and, from word 16 on, the one with its bands' scale.  (One array: the compiler
     // waits for loads on their way to an array of scales in front of every read of it.)
     __shared__ u32x4 lds[STAGES][PIECES * 64 + WAVES * 16];

@@ -70,29 +70,37 @@ void launch_product(const ScaledArgs& a, hipStream_t s) {
             case 4: return launch_ready<4, FP32>(a, s);
             default: return launch_ready<5, FP32>(a, s);
         }
-    // The block that is through first: rounds of the chip times what a step of 128 columns takes with a workgroup (of the 128 x 128 of four waves: two)
-    // on every compute unit.  The steps were measured on 8192^3 and, the two small blocks, on 300 and 100 rows of 4096 x 4096, where a step is
-    // mostly waiting and one workgroup a unit all there is.  16-bit outputs: 999 rows, 12288 x 4096: 256 x 256 52 us, 128 x 256 67, 128 x 128 69;
-    // 5120 x 13824: 173, 101, 108; 300 rows, 4096 x 4096: 64 x 128 17 us, 128 x 128 24; 100 rows: 64 x 64 14 us, 64 x 128 17.
+    // The block that is through first: rounds of the chip times what a step of 128 columns takes with as many workgroups on every compute unit as fit,
+    // or with one where there are not more.  The steps were measured on 4096 columns of 4111 rows x 28672, 999 x 12288, 700 x 5120, 300 and 100 x 4096.
+    // us, 16-bit outputs: 999 rows, 12288 x 4096: 192 x 256 48, 256 x 256 54, 128 x 256 67; 5120 x 13824: 160 x 128 76, 192 x 128 88, 128 x 256 102;
+    // 700 rows, 5120 x 4096: 128 x 128 of eight waves 22, of four 32; 300 rows, 4096 x 4096: 64 x 128 17, 128 x 128 20; 100 rows: 64 x 64 14, 64 x 128 17.
     struct Block {
         int bands, tiles, a_unit;
-        double narrow, wide;  // us a step; wide: fp32 outputs (256 x 256 has no LDS for them)
+        double narrow, wide, narrow_alone, wide_alone;  // us a step; wide: fp32 outputs (256 x 256 has no LDS for them, 128 x 256 and 64 x 128 are never the first)
     };
-    constexpr Block blocks[] = {{16, 16, 1, 1.70, 1e9}, {8, 16, 1, 1.03, 1.85}, {8, 8, 2, 1.05, 1.80}, {8, 8, 1, 0.60, 1.10}, {4, 8, 1, 0.42, 0.60}, {4, 4, 1, 0.35, 0.59}};
+    constexpr Block blocks[] = {{16, 16, 1, 1.70, 1e9, 1.70, 1e9}, {12, 16, 1, 1.48, 2.55, 1.48, 2.55}, {8, 16, 1, 1.08, 1e9, 1.08, 1e9},   {8, 8, 2, 1.09, 1.72, 1.00, 1.19},
+                                {12, 8, 1, 0.94, 1.60, 0.94, 1.60}, {8, 12, 1, 0.92, 1.60, 0.92, 1.60},  {10, 8, 1, 0.77, 1.30, 0.77, 1.30}, {8, 8, 1, 0.66, 1.08, 0.66, 1.08},
+                                {4, 8, 2, 0.69, 1e9, 0.52, 1e9},   {4, 4, 2, 0.55, 0.65, 0.44, 0.67}};
     int best = 0;
     double least = 1e18;
-    for (int i = 0; i < 6; ++i) {
-        const int at_once = 256 * blocks[i].a_unit;
-        const double t = ((blocks_of(a, blocks[i].bands, blocks[i].tiles) + at_once - 1) / at_once) * (FP32 ? blocks[i].wide : blocks[i].narrow);
+    for (int i = 0; i < 10; ++i) {
+        const Block& k = blocks[i];
+        const int n = blocks_of(a, k.bands, k.tiles), at_once = 256 * k.a_unit;
+        const double t = n <= 256 ? (FP32 ? k.wide_alone : k.narrow_alone) : ((n + at_once - 1) / at_once) * (FP32 ? k.wide : k.narrow);
         if (t < least) least = t, best = i;
     }
-    if constexpr (!FP32)
+    if constexpr (!FP32) {
         if (best == 0) return launch_block<8, 4, 2, 4, 2, FP32>(a, s);
+        if (best == 2) return launch_block<4, 4, 2, 4, 3, FP32>(a, s);
+        if (best == 8) return launch_block<2, 4, 2, 2, 3, FP32>(a, s);
+    }
     switch (best) {
-        case 1: return launch_block<4, 4, 2, 4, 3, FP32>(a, s);
-        case 2: return launch_block<4, 4, 2, 2, 2, FP32>(a, s);
-        case 3: return launch_block<2, 4, 4, 2, 4, FP32>(a, s);
-        case 4: return launch_block<2, 4, 2, 2, 3, FP32>(a, s);
+        case 1: return launch_block<4, 4, 3, 4, 2, FP32>(a, s);
+        case 3: return launch_block<4, 4, 2, 2, 2, FP32>(a, s);
+        case 4: return launch_block<4, 4, 3, 2, 3, FP32>(a, s);
+        case 5: return launch_block<4, 4, 2, 3, 3, FP32>(a, s);
+        case 6: return launch_block<2, 4, 5, 2, 3, FP32>(a, s);
+        case 7: return launch_block<2, 4, 4, 2, 4, FP32>(a, s);
         default: return launch_block<2, 4, 2, 1, 4, FP32>(a, s);
     }
 }

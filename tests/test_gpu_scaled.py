@@ -57,7 +57,10 @@ SHAPES = [(1, 64, 128), (1, 4096, 4096), (2, 17, 32), (5, 1, 96), (8, 130, 1056)
           (49, 300, 160), (64, 4099, 512), (79, 128, 11008), (80, 640, 608), (81, 640, 608), (100, 33, 96), (128, 128, 128), (129, 1000, 1408), (257, 515, 4096),
           (600, 4099, 288), (1023, 2050, 1056),
           (100, 9000, 160), (500, 4096, 416), (999, 12290, 160), (2000, 4096, 288), (999, 5120, 416), (1500, 8200, 96), (90, 200, 4096), (128, 40000, 96),
-          (26, 96, 14784), (17, 4096, 4096), (30, 9000, 2080), (32, 20000, 96), (18, 70000, 32), (25, 8000, 2112), (40, 70000, 32), (66, 20000, 64), (50, 25000, 64)]
+          (26, 96, 14784), (17, 4096, 4096), (30, 9000, 2080), (32, 20000, 96), (18, 70000, 32), (25, 8000, 2112), (40, 70000, 32), (66, 20000, 64), (50, 25000, 64),
+          # every size of block, of 16-bit and of fp32 outputs
+          (521, 16820, 96), (399, 16512, 160), (393, 12508, 96), (258, 16706, 96), (403, 11415, 160), (259, 13643, 96), (260, 16312, 96), (129, 16565, 288),
+          (82, 16487, 416), (81, 8299, 416), (92, 109, 416)]
 
 
 @BOTH
