@@ -74,10 +74,12 @@ void launch_products(const MoeArgs& a, hipStream_t s) {
         else launch_down<W, 1, 1, 8, 1>(a, s);
     } else if (each <= 28) {
         launch_gate_up<W, 2, 4, 1>(a, s);
-        launch_down<W, 2, 4, 4, 1>(a, s);
+        if (most_active(a) * a.d > 16384) launch_down<W, 2, 4, 4, 1>(a, s);
+        else launch_down<W, 2, 1, 8, 1>(a, s);
     } else {
         launch_gate_up<W, 3, 4, 1>(a, s);
-        launch_down<W, 3, 4, 4, 1>(a, s);
+        if (most_active(a) * a.d > 16384) launch_down<W, 3, 4, 4, 1>(a, s);
+        else launch_down<W, 3, 1, 8, 1>(a, s);
     }
 }
 

@@ -12,6 +12,8 @@ struct ScaledArgs {
     size_t w_scales, x_scales;  // bytes in front of the scales
     int64_t x_stride, y_stride;
     int rows, N, K, KB, row_tiles;
+    int split_blocks;      // scaled_block_kernel: blocks of columns of a workgroup; those of split s put their sums at y + s * y_split
+    int64_t y_split;
 };
 
 // Scales of rows: byte + 127 of (block j, row tile, row c of it), so that one word holds a row's place in four tiles, as the matrix instruction picks them.
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(256) void scaled_rows_kernel(ScaledArgs a) {
 // results of random rows, where their rounding to bf16 takes 1.7e-3.  That is not enough for fp32 outputs, which use the 16-bit instruction on values that
 // were converted with their scales, exactly, at half the rate.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-template <int WB, int WM, int GB, int GM, int STAGES, bool FP32>
+template <int WB, int WM, int GB, int GM, int STAGES, bool EXACT, bool FP32>
 __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a) {
     constexpr int WAVES = GB * GM, BB = WB * GB, BM = WM * GM;  // bands and row tiles of the block
     constexpr int EACH = (2 * (BB + BM) + WAVES - 1) / WAVES, PIECES = EACH * WAVES;  // the last ones may be the last tile again, for nothing
@@ -309,8 +311,9 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
     const size_t w_scale = a.w_scales + (size_t)(min(band0, band_last) >> 3) * a.KB;  // a byte for every stage, in words that are read whole
     const size_t x_step = row_scale_at(a.row_tiles, 1, 0, 0);
     const uint8_t* const word = lane < 16 ? a.xq + a.x_scales + row_scale_at(a.row_tiles, 0, min(tile0, tile_last) & ~3, c) : a.w;
+    const int j0 = blockIdx.y * a.split_blocks, j1 = min(j0 + a.split_blocks, a.KB);  // the host leaves no split empty
     auto request = [&](int j, int slot) {  // beyond the end the last one again: as many loads as ever, for the wait below
-        j = min(j, a.KB - 1);
+        j = min(j, j1 - 1);
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[i] + (size_t)j * (SCALED_TILE / 16)),
@@ -330,9 +333,9 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[b][m][i] = 0.f;
 #pragma unroll
-    for (int j = 0; j + 1 < STAGES; ++j) request(j, j);
+    for (int j = 0; j + 1 < STAGES; ++j) request(j0 + j, j);
     int slot = 0;
-    for (int j = 0; j < a.KB; ++j) {
+    for (int j = j0; j < j1; ++j) {
         __builtin_amdgcn_s_waitcnt(WAIT);  // this wave's pieces of stage j have landed
         __builtin_amdgcn_s_barrier();      // and everybody's; nobody reads stage j - 1 any more
         const uint32_t* const scales = reinterpret_cast<const uint32_t*>(&lds[slot][PIECES * 64 + wave * 16]);
@@ -361,7 +364,7 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
                 const i32x8 w = next;
                 const int t = h * (WB / 2) + b + 1;
                 if (t < WB) next = operand(ws + t % (WB / 2) * 256 + t / (WB / 2) * 64);
-                if constexpr (FP32) {
+                if constexpr (EXACT) {
                     const float fw = scale_of(sw), fx[2] = {scale_of(sx & 255), scale_of(sx >> 16 & 255)};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -403,7 +406,7 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
             const int r = i * ROWS + lane / CHUNKS, row = (tile0 + 2 * m) * 16 + r;
             const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * PITCH + lane % CHUNKS * 16);
             if (row < a.rows && n < a.N) {
-                char* y = static_cast<char*>(a.y) + ((size_t)row * a.y_stride + n) * BYTES;
+                char* y = static_cast<char*>(a.y) + ((size_t)blockIdx.y * a.y_split + (size_t)row * a.y_stride + n) * BYTES;
                 if (n + 16 / BYTES <= a.N) *reinterpret_cast<u32x4*>(y) = v;
                 else if constexpr (FP32)
                     for (int k = 0; k < a.N - n; ++k) reinterpret_cast<uint32_t*>(y)[k] = v[k];
@@ -413,4 +416,17 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
         }
         __builtin_amdgcn_wave_barrier();  // LDS serves a wave's accesses in order: the next rows' writes follow these reads
     }
+}
+
+// Where few blocks would go through many columns the columns are split, and the parts' sums, [splits][rows][part_stride], added here in their order: a
+// thread four outputs of a row.
+template <bool FP32>
+__global__ __launch_bounds__(256) void scaled_join_kernel(ScaledArgs a, const float* __restrict__ part, int splits, int part_stride) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, split = (int64_t)a.rows * part_stride;
+    const int quads = part_stride >> 2, row = (int)(i / quads), n = (int)(i - (int64_t)row * quads) * 4;
+    if (row >= a.rows) return;
+    const float* p = part + (int64_t)row * part_stride + n;
+    f32x4 v = *reinterpret_cast<const f32x4*>(p);
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * split);
+    store_outputs<FP32>(a, row, n, v);
 }

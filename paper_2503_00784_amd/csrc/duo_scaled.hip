@@ -51,12 +51,90 @@ void launch_ready(const ScaledArgs& a, hipStream_t s) {
     else launch_bands<MT, 4, 1, 2, true, FP32>(a, s);
 }
 
-int blocks_of(const ScaledArgs& a, int bands, int tiles) { return (scaled_blocks(a.N) * 8 + bands - 1) / bands * ((a.row_tiles + tiles - 1) / tiles); }
-template <int WB, int WM, int GB, int GM, int STAGES, bool FP32>
-void launch_block(const ScaledArgs& a, hipStream_t s) {
-    const int blocks = blocks_of(a, WB * GB, WM * GM);
+// ---- more than DUO_MAX_ROWS rows: which block, and over how many workgroups the columns are split.
+struct BlockPlan {
+    int block, splits;
+};
+size_t part_stride(int N) { return ((size_t)N + 3) / 4 * 4; }
+
+// What is through first: rounds of the chip times what a step of 128 columns takes with as many workgroups on every compute unit as fit, or with one
+// where there are not more; and, where the columns are split, the launch that adds up the parts.  The steps were measured on 4096 columns of
+// 4111 rows x 28672, 999 x 12288, 700 x 5120, 300 and 100 x 4096.
+// us, 16-bit outputs: 999 rows, 12288 x 4096: 192 x 256 48, 256 x 256 54, 128 x 256 67; 5120 x 13824: 160 x 128 76, 192 x 128 88, 128 x 256 102;
+// 700 rows, 5120 x 4096: 128 x 128 of eight waves 22, of four 32; 300 rows, 4096 x 4096: 64 x 128 17, 128 x 128 20; 100 rows: 64 x 64 14, 64 x 128 17.
+BlockPlan plan_blocks(int rows, int N, int K, bool fp32) {
+    struct Block {
+        int bands, tiles, a_unit;
+        double narrow, wide, narrow_alone, wide_alone;  // us a step; wide: fp32 outputs (256 x 256 has no LDS for them, 128 x 256 and 64 x 128 are never the first)
+        bool can_split;
+    };
+    static constexpr Block blocks[] = {{16, 16, 1, 1.70, 1e9, 1.70, 1e9, false},   {12, 16, 1, 1.48, 2.55, 1.48, 2.55, false}, {8, 16, 1, 1.08, 1e9, 1.08, 1e9, false},
+                                       {8, 8, 2, 1.09, 1.72, 1.00, 1.19, false},   {12, 8, 1, 0.94, 1.60, 0.94, 1.60, false},  {8, 12, 1, 0.92, 1.60, 0.92, 1.60, false},
+                                       {10, 8, 1, 0.77, 1.30, 0.77, 1.30, false},  {8, 8, 1, 0.66, 1.08, 0.66, 1.08, true},    {4, 8, 2, 0.69, 1e9, 0.52, 1e9, true},
+                                       {4, 4, 2, 0.55, 0.65, 0.44, 0.67, true}};
+    const int bands = scaled_blocks(N) * 8, tiles = (rows + 15) / 16, KB = scaled_blocks(K);
+    BlockPlan best{0, 1};
+    double least = 1e18;
+    for (int i = 0; i < 10; ++i) {
+        const Block& k = blocks[i];
+        const int n = (bands + k.bands - 1) / k.bands * ((tiles + k.tiles - 1) / k.tiles), at_once = 256 * k.a_unit;
+        for (int splits = 1; splits <= (k.can_split && n <= 256 ? 8 : 1) && (splits == 1 || KB >= 4 * splits); splits *= 2) {
+            const int m = n * splits;
+            const double step = m <= 256 ? (fp32 ? k.wide_alone : k.narrow_alone) : ((m + at_once - 1) / at_once) * (fp32 ? k.wide : k.narrow);
+            const double t = step * ((KB + splits - 1) / splits) + (splits > 1 ? 4.0 + 8e-6 / 4.0 * splits * rows * (double)N : 0.0);  // parts at 4 TB/s, written and read
+            if (t < least) least = t, best = BlockPlan{i, splits};
+        }
+    }
+    const int each = (KB + best.splits - 1) / best.splits;
+    best.splits = (KB + each - 1) / each;  // none is empty
+    return best;
+}
+size_t part_bytes(int rows, int N, int K, bool fp32) {
+    if (rows <= DUO_MAX_ROWS) return 0;
+    const BlockPlan p = plan_blocks(rows, N, K, fp32);
+    return p.splits > 1 ? (size_t)p.splits * rows * part_stride(N) * 4 : 0;
+}
+size_t workspace_of(int rows, int N, int K) {  // for either type of outputs
+    const size_t narrow = part_bytes(rows, N, K, false), wide = part_bytes(rows, N, K, true);
+    return ((rows_bytes(rows, K) + 15) & ~(size_t)15) + (narrow > wide ? narrow : wide);
+}
+
+template <int WB, int WM, int GB, int GM, int STAGES, bool EXACT, bool FP32>
+void launch_block(const ScaledArgs& a, int splits, hipStream_t s) {
+    const int blocks = (scaled_blocks(a.N) * 8 + WB * GB - 1) / (WB * GB) * ((a.row_tiles + WM * GM - 1) / (WM * GM));
     duo_internal_prof(DUO_PROF_SCALED);
-    DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, STAGES, FP32>), dim3((blocks + 7) / 8 * 8), dim3(64 * GB * GM), s, a);
+    DUO_LAUNCH((scaled_block_kernel<WB, WM, GB, GM, STAGES, EXACT, FP32>), dim3((blocks + 7) / 8 * 8, splits), dim3(64 * GB * GM), s, a);
+}
+template <bool FP32>
+void launch_blocks(ScaledArgs a, hipStream_t s) {
+    const BlockPlan p = plan_blocks(a.rows, a.N, a.K, FP32);
+    a.split_blocks = (a.KB + p.splits - 1) / p.splits, a.y_split = 0;
+    if (p.splits > 1) {
+        ScaledArgs b = a;
+        float* const part = reinterpret_cast<float*>(a.xq + ((rows_bytes(a.rows, a.K) + 15) & ~(size_t)15));
+        b.y = part, b.y_stride = (int64_t)part_stride(a.N), b.y_split = b.y_stride * a.rows;
+        if (p.block == 7) launch_block<2, 4, 4, 2, 4, FP32, true>(b, p.splits, s);
+        else if (p.block == 9) launch_block<2, 4, 2, 1, 4, FP32, true>(b, p.splits, s);
+        else if constexpr (!FP32) launch_block<2, 4, 2, 2, 3, FP32, true>(b, p.splits, s);
+        const int64_t quads = (int64_t)a.rows * (b.y_stride / 4);
+        duo_internal_prof(DUO_PROF_SCALED);
+        DUO_LAUNCH((scaled_join_kernel<FP32>), dim3((unsigned)((quads + 255) / 256)), dim3(256), s, a, part, p.splits, (int)b.y_stride);
+        return;
+    }
+    if constexpr (!FP32) {
+        if (p.block == 0) return launch_block<8, 4, 2, 4, 2, FP32, FP32>(a, 1, s);
+        if (p.block == 2) return launch_block<4, 4, 2, 4, 3, FP32, FP32>(a, 1, s);
+        if (p.block == 8) return launch_block<2, 4, 2, 2, 3, FP32, FP32>(a, 1, s);
+    }
+    switch (p.block) {
+        case 1: return launch_block<4, 4, 3, 4, 2, FP32, FP32>(a, 1, s);
+        case 3: return launch_block<4, 4, 2, 2, 2, FP32, FP32>(a, 1, s);
+        case 4: return launch_block<4, 4, 3, 2, 3, FP32, FP32>(a, 1, s);
+        case 5: return launch_block<4, 4, 2, 3, 3, FP32, FP32>(a, 1, s);
+        case 6: return launch_block<2, 4, 5, 2, 3, FP32, FP32>(a, 1, s);
+        case 7: return launch_block<2, 4, 4, 2, 4, FP32, FP32>(a, 1, s);
+        default: return launch_block<2, 4, 2, 1, 4, FP32, FP32>(a, 1, s);
+    }
 }
 
 template <bool FP32>
@@ -70,39 +148,7 @@ void launch_product(const ScaledArgs& a, hipStream_t s) {
             case 4: return launch_ready<4, FP32>(a, s);
             default: return launch_ready<5, FP32>(a, s);
         }
-    // The block that is through first: rounds of the chip times what a step of 128 columns takes with as many workgroups on every compute unit as fit,
-    // or with one where there are not more.  The steps were measured on 4096 columns of 4111 rows x 28672, 999 x 12288, 700 x 5120, 300 and 100 x 4096.
-    // us, 16-bit outputs: 999 rows, 12288 x 4096: 192 x 256 48, 256 x 256 54, 128 x 256 67; 5120 x 13824: 160 x 128 76, 192 x 128 88, 128 x 256 102;
-    // 700 rows, 5120 x 4096: 128 x 128 of eight waves 22, of four 32; 300 rows, 4096 x 4096: 64 x 128 17, 128 x 128 20; 100 rows: 64 x 64 14, 64 x 128 17.
-    struct Block {
-        int bands, tiles, a_unit;
-        double narrow, wide, narrow_alone, wide_alone;  // us a step; wide: fp32 outputs (256 x 256 has no LDS for them, 128 x 256 and 64 x 128 are never the first)
-    };
-    constexpr Block blocks[] = {{16, 16, 1, 1.70, 1e9, 1.70, 1e9}, {12, 16, 1, 1.48, 2.55, 1.48, 2.55}, {8, 16, 1, 1.08, 1e9, 1.08, 1e9},   {8, 8, 2, 1.09, 1.72, 1.00, 1.19},
-                                {12, 8, 1, 0.94, 1.60, 0.94, 1.60}, {8, 12, 1, 0.92, 1.60, 0.92, 1.60},  {10, 8, 1, 0.77, 1.30, 0.77, 1.30}, {8, 8, 1, 0.66, 1.08, 0.66, 1.08},
-                                {4, 8, 2, 0.69, 1e9, 0.52, 1e9},   {4, 4, 2, 0.55, 0.65, 0.44, 0.67}};
-    int best = 0;
-    double least = 1e18;
-    for (int i = 0; i < 10; ++i) {
-        const Block& k = blocks[i];
-        const int n = blocks_of(a, k.bands, k.tiles), at_once = 256 * k.a_unit;
-        const double t = n <= 256 ? (FP32 ? k.wide_alone : k.narrow_alone) : ((n + at_once - 1) / at_once) * (FP32 ? k.wide : k.narrow);
-        if (t < least) least = t, best = i;
-    }
-    if constexpr (!FP32) {
-        if (best == 0) return launch_block<8, 4, 2, 4, 2, FP32>(a, s);
-        if (best == 2) return launch_block<4, 4, 2, 4, 3, FP32>(a, s);
-        if (best == 8) return launch_block<2, 4, 2, 2, 3, FP32>(a, s);
-    }
-    switch (best) {
-        case 1: return launch_block<4, 4, 3, 4, 2, FP32>(a, s);
-        case 3: return launch_block<4, 4, 2, 2, 2, FP32>(a, s);
-        case 4: return launch_block<4, 4, 3, 2, 3, FP32>(a, s);
-        case 5: return launch_block<4, 4, 2, 3, 3, FP32>(a, s);
-        case 6: return launch_block<2, 4, 5, 2, 3, FP32>(a, s);
-        case 7: return launch_block<2, 4, 4, 2, 4, FP32>(a, s);
-        default: return launch_block<2, 4, 2, 1, 4, FP32>(a, s);
-    }
+    launch_blocks<FP32>(a, s);
 }
 
 }  // namespace
@@ -123,7 +169,7 @@ extern "C" int duo_scaled_workspace_bytes(int rows, int N, int K, size_t* bytes)
     if (!bytes) return DUO_ERR_NULL;
     if (const int rc = check_matrix(N, K)) return rc;
     if (rows < 1 || rows > DUO_SCALED_MAX_ROWS) return DUO_ERR_SHAPE;
-    *bytes = rows_bytes(rows, K);
+    *bytes = workspace_of(rows, N, K);
     return DUO_OK;
 }
 
@@ -140,7 +186,7 @@ extern "C" int duo_scaled_gemm(const uint16_t* x, int64_t x_stride, const void* 
     const int64_t last = rows - 1;
     const char *x1 = x0 + 2 * (last * x_stride + K), *y1 = y0 + (y_fp32 ? 4 : 2) * (last * y_stride + N), *w1 = w0 + scaled_bytes(N, K);
     if ((y0 < x1 && x0 < y1) || (y0 < w1 && w0 < y1)) return DUO_ERR_ARG;
-    const size_t need = rows_bytes(rows, K);
+    const size_t need = workspace_of(rows, N, K);
     if (need) {
         if (!workspace) return DUO_ERR_NULL;
         if (off16(workspace)) return DUO_ERR_ALIGN;

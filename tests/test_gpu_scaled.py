@@ -60,7 +60,10 @@ SHAPES = [(1, 64, 128), (1, 4096, 4096), (2, 17, 32), (5, 1, 96), (8, 130, 1056)
           (26, 96, 14784), (17, 4096, 4096), (30, 9000, 2080), (32, 20000, 96), (18, 70000, 32), (25, 8000, 2112), (40, 70000, 32), (66, 20000, 64), (50, 25000, 64),
           # every size of block, of 16-bit and of fp32 outputs
           (521, 16820, 96), (399, 16512, 160), (393, 12508, 96), (258, 16706, 96), (403, 11415, 160), (259, 13643, 96), (260, 16312, 96), (129, 16565, 288),
-          (82, 16487, 416), (81, 8299, 416), (92, 109, 416)]
+          (82, 16487, 416), (81, 8299, 416), (92, 109, 416),
+          # columns split over two, four and eight workgroups
+          (8221, 65, 5344), (4112, 65, 3456), (1037, 142, 4064), (1035, 133, 2560), (533, 133, 4224), (142, 4510, 5280), (87, 69, 2176), (94, 65, 4448),
+          (2192, 141, 2848), (2170, 73, 6016), (99, 73, 1728), (120, 1699, 12224)]
 
 
 @BOTH
@@ -76,10 +79,10 @@ def test_products(rows, N, K, fp32, dtype):
 
 
 @BOTH
-@pytest.mark.parametrize("rows", [3, 33, 130])
+@pytest.mark.parametrize("rows,K", [(3, 224), (33, 224), (130, 224), (90, 4448)])
 @pytest.mark.parametrize("fp32", [True, False])
-def test_rows_apart_and_what_lies_between_them(rows, fp32, dtype):
-    N, K = 203, 224
+def test_rows_apart_and_what_lies_between_them(rows, K, fp32, dtype):
+    N = 203
     t = torch.float32 if fp32 else U.TYPES[dtype]
     wide = _randn((rows, 3 * K), dtype, 5)
     x = wide[:, K:2 * K]
@@ -128,9 +131,9 @@ def test_no_rows():
 
 
 @BOTH
-@pytest.mark.parametrize("rows", [9, 200])
-def test_captured_and_replayed_beside_eager_calls(rows, dtype):
-    N, K = 300, 512
+@pytest.mark.parametrize("rows,K", [(9, 512), (200, 512), (100, 4096)])
+def test_captured_and_replayed_beside_eager_calls(rows, K, dtype):
+    N = 300
     w = _randn((N, K), dtype, 2)
     m = B.ScaledMatrix(w)
     x, out = _randn((rows, K), dtype, 1), torch.zeros((rows, 304), dtype=U.TYPES[dtype], device=DEV)[:, :N]
