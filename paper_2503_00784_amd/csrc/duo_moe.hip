@@ -59,6 +59,14 @@ void launch_down(const MoeArgs& a, hipStream_t s) {
     duo_internal_prof(DUO_PROF_MOE_DOWN);
     DUO_LAUNCH(moe_combine_kernel, dim3((a.d + 1023) / 1024, a.rows), dim3(256), s, a);
 }
+// Experts of two or three tiles of rows.  us with four bands for four waves, two for eight, one for eight: 60 rows, 4 of 8 experts, 4096 x 2048: 29, 48, 84;
+// 64 rows, 2 of 4 experts, 2048 x 2816: 26, 19, 31; 32 rows, 2 experts of 896 x 6816 (two tiles): 35, 33, 29.
+template <class W, int MT>
+void launch_down_tiles(const MoeArgs& a, hipStream_t s) {
+    if (most_active(a) * a.d > 12288) launch_down<W, MT, 4, 4, 1>(a, s);
+    else if (most_active(a) * a.d > 4096) launch_down<W, MT, 2, 8, 1>(a, s);
+    else launch_down<W, MT, 1, 8, 1>(a, s);
+}
 // By the rows an expert has where all have as many.  Up to 12 hardly an expert has more than 16, and one tile of rows it is, twice over a matrix where
 // one has: 80 rows, two choices of 8 experts (20 each) 102 us like this, 68 with two tiles; of 16 (10 each) 50, 52.  40 rows each: two tiles 29 us,
 // three 21, five 22.
@@ -74,12 +82,10 @@ void launch_products(const MoeArgs& a, hipStream_t s) {
         else launch_down<W, 1, 1, 8, 1>(a, s);
     } else if (each <= 28) {
         launch_gate_up<W, 2, 4, 1>(a, s);
-        if (most_active(a) * a.d > 16384) launch_down<W, 2, 4, 4, 1>(a, s);
-        else launch_down<W, 2, 1, 8, 1>(a, s);
+        launch_down_tiles<W, 2>(a, s);
     } else {
         launch_gate_up<W, 3, 4, 1>(a, s);
-        if (most_active(a) * a.d > 16384) launch_down<W, 3, 4, 4, 1>(a, s);
-        else launch_down<W, 3, 1, 8, 1>(a, s);
+        launch_down_tiles<W, 3>(a, s);
     }
 }
 

@@ -40,7 +40,8 @@ def check(layer, router, held, x, got, rows=None):
 SHAPES = [(1, 64, 32, 1, 1), (4, 128, 96, 1, 3), (8, 64, 160, 2, 16), (5, 192, 128, 5, 17), (16, 256, 64, 4, 33), (3, 512, 416, 2, 47), (64, 128, 32, 6, 64),
           (2, 320, 288, 1, 80), (512, 64, 32, 16, 80), (130, 64, 64, 8, 79), (8, 1024, 1408, 2, 9), (40, 64, 32, 3, 1), (4, 4096, 256, 2, 5), (6, 64, 4352, 2, 7),
           (32, 64, 64, 16, 17), (33, 128, 32, 16, 31), (17, 192, 32, 3, 33), (2, 64, 128, 1, 80), (3, 64, 96, 3, 80),
-          (6, 1024, 96, 3, 9), (2, 320, 1120, 1, 2), (40, 512, 64, 1, 12), (5, 2048, 64, 4, 30), (12, 1536, 64, 4, 50), (4, 4160, 64, 2, 60)]
+          (6, 1024, 96, 3, 9), (2, 320, 1120, 1, 2), (40, 512, 64, 1, 12), (5, 2048, 64, 4, 30), (12, 1536, 64, 4, 50), (4, 4160, 64, 2, 60),
+          (4, 2048, 416, 2, 64), (5, 1600, 1120, 2, 40)]
 
 
 @BOTH
