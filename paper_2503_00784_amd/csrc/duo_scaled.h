@@ -322,8 +322,8 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(word + (lane < 16 ? of_rows : of_bands)),
                                          (__attribute__((address_space(3))) void*)(&lds[slot][PIECES * 64 + wave * 16]), 4, 0, 0);
     };
-    // vmcnt: all but the youngest STAGES - 2 requests have landed (expcnt and lgkmcnt fields at their maxima)
-    constexpr int YOUNGER = (STAGES - 2) * (EACH + 1), WAIT = (YOUNGER & 15) | ((YOUNGER >> 4) << 14) | (7 << 4) | (15 << 8);
+    // vmcnt: all but the youngest STAGES - 2 requests have landed; lgkmcnt(0): this wave has read its last stage (expcnt field at its maximum)
+    constexpr int YOUNGER = (STAGES - 2) * (EACH + 1), WAIT = (YOUNGER & 15) | ((YOUNGER >> 4) << 14) | (7 << 4);
     static_assert(YOUNGER <= 63, "the counter's range");
     f32x16 acc[WB / 2][WM / 2];
 #pragma unroll
@@ -338,6 +338,7 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
     for (int j = j0; j < j1; ++j) {
         __builtin_amdgcn_s_waitcnt(WAIT);  // this wave's pieces of stage j have landed
         __builtin_amdgcn_s_barrier();      // and everybody's; nobody reads stage j - 1 any more
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);  // to the compiler: no read of this stage is older than that
         const uint32_t* const scales = reinterpret_cast<const uint32_t*>(&lds[slot][PIECES * 64 + wave * 16]);
         const int sx = (int)(scales[c] >> (8 * odd));  // byte 0: the lane's row of the first two row tiles, byte 2: of the others
         const int sw = (int)(scales[16] >> (8 * ((w_scale + j) & 3)) & 255u);
@@ -383,8 +384,9 @@ __global__ __launch_bounds__(64 * GB * GM) void scaled_block_kernel(ScaledArgs a
     // lane: feature 8 (i / 4) + 4 half + i % 4 of two bands, row l % 32.
     constexpr int BYTES = FP32 ? 4 : 2, ROW = WB * 16 * BYTES, PITCH = ROW + 16, CHUNKS = ROW / 16, ROWS = 64 / CHUNKS;  // ROWS in one store
     static_assert(sizeof(lds) >= (size_t)WAVES * 32 * PITCH, "32 rows of every wave");
-    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): nothing is on its way to LDS any more,
-    __builtin_amdgcn_s_barrier();                      // and nobody reads a stage (every wave's reads have gone into products)
+    __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0): nothing is on its way to LDS any more; lgkmcnt(0),
+    __builtin_amdgcn_s_barrier();        // and nobody reads a stage
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
     char* const mine = reinterpret_cast<char*>(&lds[0][0]) + wave * 32 * PITCH;
     const int n = band0 * 16 + lane % CHUNKS * (16 / BYTES);
 #pragma unroll
