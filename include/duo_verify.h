@@ -522,7 +522,10 @@ int duo_stream_read_probe(const void *src, size_t bytes, uint32_t *sink, int sin
  * about 260); duo_profile_dropped returns how many launches since the last read (or enable) found the pool
  * empty and went untimed -- call it before duo_profile_read, which resets it.  A call made while profiling is
  * not allocation-free or capturable.  Not thread-safe.
- * ms and launches are HOST arrays of DUO_PROF_CLASSES entries.
+ * ms and launches are HOST arrays: of DUO_PROF_CLASSES entries for duo_profile_read, which reports the classes below that and leaves out what was
+ * launched under the others; of `classes` entries (1 or more, else DUO_ERR_ARG) for duo_profile_read_classes, which reports as many, DUO_PROF_ALL_CLASSES
+ * being all there are (entries behind them receive zero).  Classes that are added later raise DUO_PROF_ALL_CLASSES alone: a program that was built
+ * before them hands over arrays as long as they have to be.  Either call resets the sums of all classes.
  */
 #define DUO_PROF_SETUP     0  /* rotary table, embedding gather + first RMSNorm, input checks, root statistics; duo_page_plan */
 #define DUO_PROF_QKV       1  /* fused QKV projection + rotary + KV scatter */
@@ -536,13 +539,15 @@ int duo_stream_read_probe(const void *src, size_t bytes, uint32_t *sink, int sin
 #define DUO_PROF_SAMPLE    9  /* softmax statistics, accept tests, correction/bonus sampling */
 #define DUO_PROF_COMMIT    10 /* sequence selection + KV commit; duo_page_commit */
 #define DUO_PROF_QKV_FINISH 11 /* 49 rows and more: sum of the K-split Q/K/V partial results + rotary + KV scatter; duo_page_append */
+#define DUO_PROF_CLASSES    12 /* entries of duo_profile_read */
 #define DUO_PROF_SCALED     12 /* duo_scaled_gemm */
 #define DUO_PROF_MOE_ROUTER 13 /* duo_moe_layer: logits, choice of experts */
 #define DUO_PROF_MOE_GATEUP 14 /* duo_moe_layer: gate/up products + SwiGLU */
 #define DUO_PROF_MOE_DOWN   15 /* duo_moe_layer: down product, sum over a row's experts */
-#define DUO_PROF_CLASSES    16
+#define DUO_PROF_ALL_CLASSES 16
 int duo_profile_enable(int enable);
 int duo_profile_read(double *ms, int32_t *launches);
+int duo_profile_read_classes(double *ms, int32_t *launches, int classes);
 int duo_profile_dropped(void);
 /* Name, with template arguments as a kernel trace prints them, of the projection kernel most recently launched under
  * class `cls` while the timer was enabled ("" if none, or if that class's kernels are not named); HOST string, valid until

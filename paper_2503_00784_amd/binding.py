@@ -34,7 +34,7 @@ EXPORTS = ["duo_workspace_bytes", "duo_verify", "duo_prefill_chunk", "duo_sample
            "duo_spec_sample", "duo_spec_sample_noalloc", "duo_verify_deferred", "duo_deferred_sample", "duo_skinny_gemm",
            "duo_block_gemm", "duo_stream_read_probe", "duo_k_cache_offset",
            "duo_v_cache_offset", "duo_status_string", "duo_last_hip_error", "duo_profile_enable",
-           "duo_profile_read", "duo_profile_dropped", "duo_profile_kernel_name", "duo_packed_elems", "duo_pack_matrix", "duo_pack_qkv", "duo_pack_gate_up",
+           "duo_profile_read", "duo_profile_read_classes", "duo_profile_dropped", "duo_profile_kernel_name", "duo_packed_elems", "duo_pack_matrix", "duo_pack_qkv", "duo_pack_gate_up",
            "duo_pack_activations",
            "duo_page_workspace_bytes", "duo_page_plan", "duo_page_append", "duo_page_attention", "duo_page_commit",
            "duo_scaled_bytes", "duo_scaled_pack", "duo_scaled_workspace_bytes", "duo_scaled_gemm",
@@ -178,7 +178,8 @@ def load(dtype: str = "bf16") -> C.CDLL:
     lib.duo_profile_enable.argtypes = [C.c_int]
     lib.duo_profile_enable.restype = C.c_int
     lib.duo_profile_read.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int32)]
-    lib.duo_profile_read.restype = C.c_int
+    lib.duo_profile_read_classes.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int32), C.c_int]
+    lib.duo_profile_read.restype = lib.duo_profile_read_classes.restype = C.c_int
     lib.duo_status_string.argtypes = [C.c_int]
     lib.duo_status_string.restype = C.c_char_p
     lib.duo_last_hip_error.argtypes = []
@@ -221,7 +222,7 @@ def profile_read(dtype: str = "bf16") -> Dict[str, Dict[str, float]]:
     n = len(PROF_CLASSES)
     ms = (C.c_double * n)()
     cnt = (C.c_int32 * n)()
-    _check(load(dtype).duo_profile_read(ms, cnt), "duo_profile_read")
+    _check(load(dtype).duo_profile_read_classes(ms, cnt, n), "duo_profile_read_classes")
     return {PROF_CLASSES[i]: {"ms": ms[i], "launches": cnt[i]} for i in range(n)}
 
 

@@ -192,7 +192,7 @@ struct Profiler {
     std::vector<int> cls;        // class of pair i
     size_t used = 0;             // pairs in use
     size_t dropped = 0;          // launches since the last read that found the pool empty
-    char names[DUO_PROF_CLASSES][128] = {};  // per class: the kernel last launched under it, as its launch helper spelled it
+    char names[DUO_PROF_ALL_CLASSES][128] = {};  // per class: the kernel last launched under it, as its launch helper spelled it
 };
 Profiler g_prof;
 constexpr size_t PROF_POOL = 8192;  // pairs
@@ -207,7 +207,7 @@ inline void prof(int cls, hipStream_t) {
     }
     g_launch_events.start = g_prof.ev[2 * g_prof.used];
     g_launch_events.stop = g_prof.ev[2 * g_prof.used + 1];
-    g_launch_events.name = cls < DUO_PROF_CLASSES ? g_prof.names[cls] : nullptr;
+    g_launch_events.name = cls < DUO_PROF_ALL_CLASSES ? g_prof.names[cls] : nullptr;
     g_prof.cls[g_prof.used] = cls;
     ++g_prof.used;
 }
@@ -939,11 +939,12 @@ int duo_profile_enable(int enable) {
 
 int duo_profile_dropped(void) { return (int)g_prof.dropped; }
 
-const char* duo_profile_kernel_name(int cls) { return (cls >= 0 && cls < DUO_PROF_CLASSES) ? g_prof.names[cls] : ""; }
+const char* duo_profile_kernel_name(int cls) { return (cls >= 0 && cls < DUO_PROF_ALL_CLASSES) ? g_prof.names[cls] : ""; }
 
-int duo_profile_read(double* ms, int32_t* launches) {
+int duo_profile_read_classes(double* ms, int32_t* launches, int classes) {
     if (!ms || !launches) return DUO_ERR_NULL;
-    for (int i = 0; i < DUO_PROF_CLASSES; ++i) {
+    if (classes < 1) return DUO_ERR_ARG;
+    for (int i = 0; i < classes; ++i) {
         ms[i] = 0.0;
         launches[i] = 0;
     }
@@ -952,6 +953,7 @@ int duo_profile_read(double* ms, int32_t* launches) {
         if (rc) return rc;
         float t = 0.f;
         if ((rc = hip_ok(hipEventElapsedTime(&t, g_prof.ev[2 * i], g_prof.ev[2 * i + 1]), "hipEventElapsedTime"))) return rc;
+        if (g_prof.cls[i] >= classes) continue;
         ms[g_prof.cls[i]] += t;
         launches[g_prof.cls[i]] += 1;
     }
@@ -959,6 +961,8 @@ int duo_profile_read(double* ms, int32_t* launches) {
     g_prof.dropped = 0;
     return DUO_OK;
 }
+
+int duo_profile_read(double* ms, int32_t* launches) { return duo_profile_read_classes(ms, launches, DUO_PROF_CLASSES); }
 
 const char* duo_status_string(int code) {
     switch (code) {
