@@ -711,6 +711,14 @@ class _OnDevice:
         if rc:
             _check(rc, function.__name__)
 
+    def _wait_for_packing(self) -> None:
+        """At the end of a constructor: calls on other streams find what it has enqueued done.  A wait of the host, once, and no event that the first
+        call on a stream waits for: that call may be a captured one, which must not wait for an event from outside its graph.  (A handle that is itself
+        made while the stream is captured belongs to that graph: nothing can be waited for.)"""
+        with self._torch.cuda.device(self._index):
+            if not self._torch.cuda.is_current_stream_capturing():
+                self._torch.cuda.current_stream().synchronize()
+
     def _matrix(self, name: str, w, N: int, K: int):
         """A weight matrix as the packing calls take it: contiguous, of the handle's type, 16-byte aligned."""
         if tuple(w.shape) != (N, K) or w.dtype != self._element or w.get_device() != self._index:
@@ -744,8 +752,8 @@ def _type_name(w) -> str:
 class ScaledMatrix(_OnDevice):
     """A matrix [N][K] held in 8-bit floating point with a power of two for every block of 128 x 128 (duo_scaled_pack), and products of rows with it.
 
-    w: bf16 or fp16 on the GPU, which decides the type of the rows (and the library build); it is not kept.  The calls go to the current stream of
-    the matrix's device and keep no state: calls on several streams, or captured ones, may run side by side."""
+    w: bf16 or fp16 on the GPU, which decides the type of the rows (and the library build); it is not kept.  The constructor waits for the packing.  The
+    calls go to the current stream of the matrix's device and keep no state: calls on several streams, or captured ones, may run side by side."""
 
     def __init__(self, w):
         if w.dim() != 2:
@@ -758,6 +766,7 @@ class ScaledMatrix(_OnDevice):
         w = self._matrix("w", w, self.N, self.K)
         self._bytes = self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
         self._call(self.lib.duo_scaled_pack, w.data_ptr(), self.N, self.K, self._bytes.data_ptr())
+        self._wait_for_packing()
         self._ptr = self._bytes.data_ptr()
         self._in, self._out = (self._element,), (self._element, self._torch.float32)
         self._gemm = self.lib.duo_scaled_gemm
@@ -807,7 +816,8 @@ class ExpertLayer(_OnDevice):
 
     router [n_experts][d_model]; experts: for every expert its gate and up [d_ff][d_model] and down [d_model][d_ff] matrices (any iterable, taken one
     expert at a time; nothing of it is kept), all bf16 or all fp16 on one GPU.  scaled: the experts are held in the 8-bit blocks of ScaledMatrix.
-    renormalise: a row's shares add up to one.  The calls go to the current stream of the layer's device and keep no state."""
+    renormalise: a row's shares add up to one.  The constructor waits for the packing; the calls go to the current stream of the layer's device and keep
+    no state."""
 
     def __init__(self, router, experts, top_k: int, scaled: bool = False, renormalise: bool = True):
         if router.dim() != 2:
@@ -835,6 +845,7 @@ class ExpertLayer(_OnDevice):
             taken += 1
         if taken != n or n == 0:
             raise ValueError(f"{taken} experts, the router has {n} rows")
+        self._wait_for_packing()
         self.n_experts, self.d_model, self.d_ff, self.top_k = n, d, ff, int(top_k)
         self.scaled, self.renormalise = bool(scaled), bool(renormalise)
         self._ref, self._router_ptr, self._experts_ptr = C.byref(self.cfg), self._router.data_ptr(), self._packed.data_ptr()
