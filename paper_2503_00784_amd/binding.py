@@ -700,9 +700,12 @@ class _OnDevice:
         self._stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.lib = load(dtype)
+        self._held, self._streams = (), {self._stream_of(self._index)}  # the device memory of the handle, the streams it is known to be used on
 
     def _call(self, function, *args) -> None:
         stream = self._stream_of(self._index)
+        if stream not in self._streams:
+            self._used_on(stream)
         if self._index == self._current():
             rc = function(*args, stream)
         else:
@@ -711,10 +714,18 @@ class _OnDevice:
         if rc:
             _check(rc, function.__name__)
 
-    def _wait_for_packing(self) -> None:
-        """At the end of a constructor: calls on other streams find what it has enqueued done.  A wait of the host, once, and no event that the first
-        call on a stream waits for: that call may be a captured one, which must not wait for an event from outside its graph.  (A handle that is itself
-        made while the stream is captured belongs to that graph: nothing can be waited for.)"""
+    def _used_on(self, stream: int) -> None:
+        """The current stream is one the handle was not used on before: without this the allocator would hand out the memory of a handle that is dropped
+        while calls on that stream are still to come.  Once a stream is enough, it is asked when the memory is released."""
+        for t in self._held:
+            t.record_stream(self._torch.cuda.current_stream(self._index))
+        self._streams.add(stream)
+
+    def _hold(self, *tensors) -> None:
+        """At the end of a constructor: what the handle's calls read.  Calls on other streams find the packing done: a wait of the host, once, and no
+        event that the first call on a stream waits for, because that call may be a captured one, which must not wait for an event from outside its
+        graph.  (A handle that is itself made while the stream is captured belongs to that graph: nothing can be waited for.)"""
+        self._held = tensors
         with self._torch.cuda.device(self._index):
             if not self._torch.cuda.is_current_stream_capturing():
                 self._torch.cuda.current_stream().synchronize()
@@ -753,7 +764,8 @@ class ScaledMatrix(_OnDevice):
     """A matrix [N][K] held in 8-bit floating point with a power of two for every block of 128 x 128 (duo_scaled_pack), and products of rows with it.
 
     w: bf16 or fp16 on the GPU, which decides the type of the rows (and the library build); it is not kept.  The constructor waits for the packing.  The
-    calls go to the current stream of the matrix's device and keep no state: calls on several streams, or captured ones, may run side by side."""
+    calls go to the current stream of the matrix's device and keep no state: calls on several streams, or captured ones, may run side by side.  A matrix
+    may be dropped while calls are on their way, on whatever stream; a graph that holds calls of it needs it as long as it is replayed."""
 
     def __init__(self, w):
         if w.dim() != 2:
@@ -766,7 +778,7 @@ class ScaledMatrix(_OnDevice):
         w = self._matrix("w", w, self.N, self.K)
         self._bytes = self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
         self._call(self.lib.duo_scaled_pack, w.data_ptr(), self.N, self.K, self._bytes.data_ptr())
-        self._wait_for_packing()
+        self._hold(self._bytes)
         self._ptr = self._bytes.data_ptr()
         self._in, self._out = (self._element,), (self._element, self._torch.float32)
         self._gemm = self.lib.duo_scaled_gemm
@@ -779,6 +791,7 @@ class ScaledMatrix(_OnDevice):
     def values(self):
         """fp32 [N][K]: what the stored values stand for."""
         torch = self._torch
+        self._used_on(self._stream_of(self._index))
         nb, kb = (self.N + 127) // 128, (self.K + 127) // 128
         tiles = nb * kb * 16384
         q = self._bytes[:tiles].view(torch.float8_e4m3fn).float().reshape(nb, 8, kb, 2, 4, 16, 16)  # row block, band, column block, half, g, row, column
@@ -817,7 +830,7 @@ class ExpertLayer(_OnDevice):
     router [n_experts][d_model]; experts: for every expert its gate and up [d_ff][d_model] and down [d_model][d_ff] matrices (any iterable, taken one
     expert at a time; nothing of it is kept), all bf16 or all fp16 on one GPU.  scaled: the experts are held in the 8-bit blocks of ScaledMatrix.
     renormalise: a row's shares add up to one.  The constructor waits for the packing; the calls go to the current stream of the layer's device and keep
-    no state."""
+    no state.  A layer may be dropped while calls are on their way; a graph that holds calls of it needs it as long as it is replayed."""
 
     def __init__(self, router, experts, top_k: int, scaled: bool = False, renormalise: bool = True):
         if router.dim() != 2:
@@ -845,7 +858,7 @@ class ExpertLayer(_OnDevice):
             taken += 1
         if taken != n or n == 0:
             raise ValueError(f"{taken} experts, the router has {n} rows")
-        self._wait_for_packing()
+        self._hold(self._router, self._packed)
         self.n_experts, self.d_model, self.d_ff, self.top_k = n, d, ff, int(top_k)
         self.scaled, self.renormalise = bool(scaled), bool(renormalise)
         self._ref, self._router_ptr, self._experts_ptr = C.byref(self.cfg), self._router.data_ptr(), self._packed.data_ptr()

@@ -109,3 +109,41 @@ def test_made_while_its_stream_is_captured(kind):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+@KINDS
+@pytest.mark.parametrize("captured", [False, True])
+def test_dropped_while_calls_are_on_their_way(kind, captured, busy):
+    """The memory of a handle is not handed out while a call on another stream than the handle's own still reads it, also where a captured call
+    was the first one there."""
+    sources, x = _sources(kind), _rows(kind)
+    handle = _handle(kind, sources)
+    want = _use(handle, x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    if captured:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            _use(handle, x)
+    held = [(t.data_ptr(), t.numel() * t.element_size()) for t in ([handle.packed] if kind == "matrix" else [handle._packed, handle._router])]
+    with torch.cuda.stream(side):
+        busy()
+        got = _use(handle, x)
+    del handle
+    others = [torch.full((n,), 0x38, dtype=torch.uint8, device=DEV) for _, n in held for _ in range(3)]
+    assert not side.query()  # what follows was asked for while the call was on its way
+    assert all(o.data_ptr() + o.numel() <= p or p + n <= o.data_ptr() for o in others for p, n in held)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_streams_are_recorded_once():
+    handle, x, side = _handle("layer", _sources("layer")), _rows("layer"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        first = _use(handle, x)
+        known = set(handle._streams)
+        again = _use(handle, x)
+    torch.cuda.synchronize()
+    assert handle._streams == known and len(known) == 2
+    assert torch.equal(first, again)
