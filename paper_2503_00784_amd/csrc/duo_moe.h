@@ -300,6 +300,15 @@ __device__ __forceinline__ void add_block(f32x4& sum, const f32x4& block, const 
     } else sum = block;
 }
 
+// h as bf16 pair hi + lo.  Magnitudes that would round to 2^128 are cut instead, and lo is zero where hi is all there is: an infinity stays one.
+__device__ __forceinline__ void hidden_pair(float h, u16& hi, u16& lo) {
+    const uint32_t bits = __float_as_uint(h);
+    const bool top = (bits & 0x7fffffffu) - 0x7f7f0001u <= 0x7f800000u - 0x7f7f0001u;  // above the largest bf16 value, infinities among them
+    hi = top ? (u16)(bits >> 16) : __builtin_bit_cast(u16, (__bf16)h);
+    const float rest = __uint_as_float((uint32_t)hi << 16);
+    lo = h == rest ? (u16)0 : __builtin_bit_cast(u16, (__bf16)(h - rest));
+}
+
 // ---- gate and up.  A workgroup owns 16 hidden channels of one expert: a band of its gate and one of its up matrix, which its waves read in turns of
 // 128 columns, PF of them on their way at any time; the sums of the waves are added through LDS in wave order.  The columns of the product are the
 // rows that chose the expert, 16 MT at a time.  Hidden values are left as bf16 pairs hi + lo (16 bits of mantissa, fp32's range in either build),
@@ -398,9 +407,7 @@ __global__ __launch_bounds__(64 * NW) void moe_gate_up_kernel(MoeArgs a) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const float h = s[q] / (1.0f + expf(-s[q])) * u[q] * share;
-                    const __bf16 b = (__bf16)h;
-                    hi[q] = __builtin_bit_cast(u16, b);
-                    lo[q] = __builtin_bit_cast(u16, (__bf16)(h - (float)b));
+                    hidden_pair(h, hi[q], lo[q]);
                 }
                 u16* dst = a.hidden + (size_t)p * 2 * a.ff_pad + band * 16 + 4 * g;
                 *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
