@@ -238,7 +238,7 @@ __device__ __forceinline__ u32x4 row_load(__amdgpu_buffer_rsrc_t r, uint32_t off
 // A band's tiles of 128 columns as operands, from a matrix in 16 bits (tiles of 16 x 32, the library's streaming layout) or in e4m3 with block
 // scales.  column(i, g): the first of the eight columns of the block that a lane of group g holds in operand i.
 struct Wide {  // 16 bits
-    static constexpr bool SCALED = false;
+    static constexpr bool SCALED = false, SCALED_SUMS = false;
     u32x4 v[4];
     static __host__ __device__ size_t bytes(int N, int K) { return (size_t)((N + 31) / 32) * 32 * K * 2; }
     static __device__ __forceinline__ int column(int i, int g) { return 32 * i + 8 * g; }
@@ -254,10 +254,16 @@ struct Wide {  // 16 bits
             if (4 * j + i >= K >> 5) v[i] = u32x4{0u, 0u, 0u, 0u};
     }
     __device__ __forceinline__ elem8 operand(int i) const { return __builtin_bit_cast(elem8, v[i]); }
-    __device__ __forceinline__ float scale() const { return 1.f; }
 };
-struct Narrow {  // e4m3; the block's scale is applied to the sums of its products
-    static constexpr bool SCALED = true;
+// e4m3.  bf16 operands are values times scale, exact.  (A scale on the sums of a block's products with the bare values, up to 448 whatever they stand for,
+// comes too late for rows and hidden values from 2^119 on.)  fp16 has no room for every scale, and its rows, below 2^16, cannot make such sums too large:
+// there it goes on the sums.
+struct Narrow {
+#ifdef DUO_FP16
+    static constexpr bool SCALED = true, SCALED_SUMS = true;
+#else
+    static constexpr bool SCALED = true, SCALED_SUMS = false;
+#endif
     u32x4 v[2];
     int byte;
     static __host__ __device__ size_t bytes(int N, int K) { return scaled_bytes(N, K); }
@@ -271,7 +277,8 @@ struct Narrow {  // e4m3; the block's scale is applied to the sums of its produc
     }
     __device__ __forceinline__ void cut(int, int) {}
     __device__ __forceinline__ uint32_t word(int i, int n) const { return v[i >> 1][2 * (i & 1) + n]; }
-    __device__ __forceinline__ elem8 operand(int i) const {  // e4m3 values without their scale: exact in either 16-bit type
+    __device__ __forceinline__ bf16x8 operand_bf16(int i) const { return e4m3_to_bf16(word(i, 0), word(i, 1), scale()); }
+    __device__ __forceinline__ elem8 operand(int i) const {
 #ifdef DUO_FP16
         union {
             f16x2 p[4];
@@ -284,16 +291,16 @@ struct Narrow {  // e4m3; the block's scale is applied to the sums of its produc
         }
         return f.v;
 #else
-        return e4m3_to_bf16(word(i, 0), word(i, 1), 1.0f);
+        return operand_bf16(i);
 #endif
     }
     __device__ __forceinline__ float scale() const { return scale_of(byte); }
 };
 
-// sum += (or, with block scales, sum += scale *) what the four operands of a block give
+// what the four operands of a block have added to the sum takes its place; where the scale is still to come, sum += scale * that
 template <class W>
 __device__ __forceinline__ void add_block(f32x4& sum, const f32x4& block, const W& w) {
-    if constexpr (W::SCALED) {
+    if constexpr (W::SCALED_SUMS) {
         const float s = w.scale();
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] = fmaf(block[i], s, sum[i]);
@@ -369,7 +376,7 @@ __global__ __launch_bounds__(64 * NW) void moe_gate_up_kernel(MoeArgs a) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                     if (first + m * 16 < count) {  // the same for every lane
-                        f32x4 sum = W::SCALED ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[b][m];
+                        f32x4 sum = W::SCALED_SUMS ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[b][m];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) sum = mfma16(o[q], __builtin_bit_cast(elem8, x[s][m][q]), sum);
                         add_block(acc[b][m], sum, w[s][b]);
@@ -432,7 +439,7 @@ struct DownOperand {
 #endif
     bf16x8 v[PARTS];
     __device__ __forceinline__ explicit DownOperand(const W& w, int i) {
-        if constexpr (W::SCALED) v[0] = e4m3_to_bf16(w.word(i, 0), w.word(i, 1), 1.0f);
+        if constexpr (W::SCALED) v[0] = w.operand_bf16(i);
         else if constexpr (PARTS == 1) v[0] = __builtin_bit_cast(bf16x8, w.v[i]);
         else {
             Frag8 f;
@@ -449,8 +456,7 @@ struct DownOperand {
 
 // sum += a block of a down matrix times hidden pairs (hi in x[0 .. 3], lo in x[4 .. 7])
 template <class W>
-__device__ __forceinline__ void down_block(f32x4& acc, const W& w, const DownOperand<W> (&o)[4], const u32x4 (&x)[8]) {
-    f32x4 sum = W::SCALED ? f32x4{0.f, 0.f, 0.f, 0.f} : acc;
+__device__ __forceinline__ void down_block(f32x4& sum, const DownOperand<W> (&o)[4], const u32x4 (&x)[8]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const bf16x8 hi = __builtin_bit_cast(bf16x8, x[q]), lo = __builtin_bit_cast(bf16x8, x[4 + q]);
@@ -458,7 +464,6 @@ __device__ __forceinline__ void down_block(f32x4& acc, const W& w, const DownOpe
         sum = mfma_bf16(o[q].v[0], lo, sum);
         if constexpr (DownOperand<W>::PARTS == 2) sum = mfma_bf16(o[q].v[DownOperand<W>::PARTS - 1], hi, sum);
     }
-    add_block(acc, sum, w);
 }
 
 // ---- down.  As gate and up: a workgroup owns NB bands of one expert, the columns are the rows that chose it; what a row gets from each of its experts
@@ -515,7 +520,7 @@ __global__ __launch_bounds__(64 * NW) void moe_down_kernel(MoeArgs a) {
                 const DownOperand<W> o[4] = {DownOperand<W>(w[s][b], 0), DownOperand<W>(w[s][b], 1), DownOperand<W>(w[s][b], 2), DownOperand<W>(w[s][b], 3)};
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
-                    if (first + m * 16 < count) down_block(acc[b][m], w[s][b], o, x[s][m]);  // the same for every lane
+                    if (first + m * 16 < count) down_block<W>(acc[b][m], o, x[s][m]);  // the same for every lane
             }
         };
 #pragma unroll

@@ -27,7 +27,7 @@ def _rows(rows, first):
     return x.to(torch.bfloat16).to(DEV)
 
 
-@pytest.mark.parametrize("scaled", [False])
+@FORMS
 @pytest.mark.parametrize("n,rows", [(1, 3), (4, 5), (1, 20), (1, 40)])
 def test_hidden_values_between_the_largest_of_bf16_and_of_fp32(n, rows, scaled):
     """(181 / 128)^2 * 2^127 is below fp32's largest number and rounds to 2^128 in bf16.  The pair keeps 2^-16 of a hidden value, and the output, of the
@@ -51,3 +51,14 @@ def test_hidden_values_beyond_fp32_are_infinite(n, top_k, rows, scaled):
     keep = [r for r in range(rows) if r != 1]
     assert torch.equal(y[keep], (sign * torch.inf).expand(len(keep), D))
     assert torch.equal(y[1], sign * 2.0 ** -30)
+
+
+@pytest.mark.parametrize("n,rows", [(1, 3), (1, 20), (1, 40)])
+@FORMS
+def test_rows_near_the_largest(n, rows, scaled):
+    """Rows of 1.5 * 2^126 under gates and ups that bring them to 1.5 * 2^26 and 1.5 * 2^24: products with what the matrices stand for, far from the end of
+    fp32, whatever scale the 8-bit blocks have (2^-100 is 256 * 2^-108 there)."""
+    layer = _layer(2.0 ** -100, 2.0 ** -102, 2.0 ** -50, n, 1, scaled)
+    y = layer.run(_rows(rows, 1.5 * 2.0 ** 126))[0].cpu().double()
+    want = 2.25 * torch.where(torch.arange(D) % 2 == 0, 1.0, -1.0).double()
+    assert torch.equal(y, want.expand(rows, D))
