@@ -307,18 +307,31 @@ __device__ __forceinline__ void add_block(f32x4& sum, const f32x4& block, const 
     } else sum = block;
 }
 
-// h as bf16 pair hi + lo.  Magnitudes that would round to 2^128 are cut instead, and lo is zero where hi is all there is: an infinity stays one.
-__device__ __forceinline__ void hidden_pair(float h, u16& hi, u16& lo) {
-    const uint32_t bits = __float_as_uint(h);
-    const bool top = (bits & 0x7fffffffu) - 0x7f7f0001u <= 0x7f800000u - 0x7f7f0001u;  // above the largest bf16 value, infinities among them
-    hi = top ? (u16)(bits >> 16) : __builtin_bit_cast(u16, (__bf16)h);
-    const float rest = __uint_as_float((uint32_t)hi << 16);
-    lo = h == rest ? (u16)0 : __builtin_bit_cast(u16, (__bf16)(h - rest));
+// h as bf16 pairs hi + lo.  Magnitudes that would round to 2^128 are cut instead, and lo is zero where hi is an infinity, which so stays one.  (In fp16
+// there is neither: sums over finite rows and matrices stay below 2^45, hidden values below 2^90.)
+__device__ __forceinline__ void hidden_pairs(const float (&h)[4], u16 (&hi)[4], u16 (&lo)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const __bf16 b = (__bf16)h[q];
+        hi[q] = __builtin_bit_cast(u16, b);
+        lo[q] = __builtin_bit_cast(u16, (__bf16)(h[q] - (float)b));
+    }
+#ifndef DUO_FP16
+    constexpr float LARGEST = 0x1.fep127f;  // of bf16
+    if (fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3]))) > LARGEST)  // (fmaxf passes over NaN, whose pair is NaN already)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (fabsf(h[q]) > LARGEST) {
+                hi[q] = (u16)(__float_as_uint(h[q]) >> 16);
+                lo[q] = fabsf(h[q]) == __builtin_huge_valf() ? (u16)0 : __builtin_bit_cast(u16, (__bf16)(h[q] - __uint_as_float((uint32_t)hi[q] << 16)));
+            }
+#endif
 }
 
 // ---- gate and up.  A workgroup owns 16 hidden channels of one expert: a band of its gate and one of its up matrix, which its waves read in turns of
-// 128 columns, PF of them on their way at any time; the sums of the waves are added through LDS in wave order.  The columns of the product are the
-// rows that chose the expert, 16 MT at a time.  Hidden values are left as bf16 pairs hi + lo (16 bits of mantissa, fp32's range in either build),
+// 128 columns, PF of them at a time: while a wave forms the products of one, PF - 1 are on their way.  With PF = 1, as for two and three tiles of rows,
+// none is: it waits a whole latency for each, and the other waves of its SIMD have to fill the gap.  The sums of the waves
+// are added through LDS in wave order.  The columns of the product are the rows that chose the expert, 16 MT at a time.  Hidden values are left as bf16 pairs hi + lo (16 bits of mantissa, fp32's range in either build),
 // with the row's share of the expert in them.
 template <class W, int MT, int NW, int PF>
 __global__ __launch_bounds__(64 * NW) void moe_gate_up_kernel(MoeArgs a) {
@@ -410,12 +423,11 @@ __global__ __launch_bounds__(64 * NW) void moe_gate_up_kernel(MoeArgs a) {
             if (at < count) {
                 const int p = rows.entry[at];
                 const float share = a.share[p];
+                float h[4];
                 u16 hi[4], lo[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float h = s[q] / (1.0f + expf(-s[q])) * u[q] * share;
-                    hidden_pair(h, hi[q], lo[q]);
-                }
+                for (int q = 0; q < 4; ++q) h[q] = s[q] / (1.0f + expf(-s[q])) * u[q] * share;
+                hidden_pairs(h, hi, lo);
                 u16* dst = a.hidden + (size_t)p * 2 * a.ff_pad + band * 16 + 4 * g;
                 *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
                 *reinterpret_cast<uint2*>(dst + a.ff_pad) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
