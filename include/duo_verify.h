@@ -451,7 +451,7 @@ int duo_scaled_gemm(const uint16_t *x, int64_t x_stride, const void *w, void *y,
  *
  * R [n_experts][d_model] row-major in 16 bits; G_e, U_e [d_ff][d_model] and D_e [d_model][d_ff] in 16 bits or (scaled = 1) in
  * the 8-bit blocks above; the rows themselves are never brought to 8 bits.  l is formed in 64 bits: equal logits are taken in ascending
- * order of the experts, NaN counts as the least.  Sums are fp32; silu(..) * (..) * g_e enters the last product as a pair of bf16 values (16
+ * order of the experts, NaN counts as minus infinity.  Sums are fp32; silu(..) * (..) * g_e enters the last product as a pair of bf16 values (16
  * bits of mantissa, fp32's range); y is rounded once.
  *
  * duo_moe_pack puts one expert (row-major matrices in 16 bits, 16-byte aligned) at its place among the n_experts *

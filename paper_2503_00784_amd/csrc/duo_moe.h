@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * LOGIT_WAVES) void moe_logits_kernel(MoeArgs a)
 }
 
 // One workgroup a row: its logits' parts added up, the rank of every expert, which is the number of experts in front of it (all at once: no search of top_k
-// rounds), and the shares.  NaN counts as the least of values; equal ones rank by their number.
+// rounds), and the shares.  NaN counts as minus infinity; equal ones rank by their number.
 constexpr int CHOICE_THREADS = 512;
 __global__ __launch_bounds__(CHOICE_THREADS) void moe_choice_kernel(MoeArgs a) {
     __shared__ double raw[MOE_MAX_EXPERTS], key[MOE_MAX_EXPERTS];

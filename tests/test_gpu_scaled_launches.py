@@ -117,3 +117,32 @@ def test_as_many_rows_as_there_can_be():
     held = U.blocks(w, True)
     for a, b in ((0, 200), (rows // 2 - 100, rows // 2 + 100), (rows - 200, rows)):
         U.close(got[a:b], *U.product(x[a:b], held, got.dtype, True), f"rows {a} to {b}")
+
+
+@OUTPUTS
+@pytest.mark.parametrize("rows,N,K", [(9, 150, 96), (20, 150, 224), (40, 150, 352), (90, 150, 96), (94, 65, 4448)])
+def test_what_lies_around_the_rows_does_not_matter(rows, N, K, fp32):
+    """NaN between the rows and behind the last one, columns that end inside a block."""
+    w, x = _randn((N, K), "bf16", 1, K ** -0.5), _randn((rows, K), "bf16", 2)
+    around = torch.full((rows, K + 72), float("nan"), dtype=torch.bfloat16, device=DEV)
+    around[:, 8:8 + K] = x
+    m = B.ScaledMatrix(w)
+    _compare(m, x, fp32, U.blocks(w, True))
+    assert torch.equal(m.product(around[:, 8:8 + K], fp32=fp32), m.product(x, fp32=fp32))
+
+
+@BOTH
+@pytest.mark.parametrize("rows,N,K", [(20, 150, 384), (40, 150, 384), (94, 150, 4448)])
+def test_infinities_and_nan_stay_in_their_row_and_their_column(rows, N, K, dtype):
+    """Where a launch of its own brings the rows to e4m3, and where the columns are split over workgroups."""
+    x, w = _randn((rows, K), dtype, 1), _randn((N, K), dtype, 2, K ** -0.5)
+    x[1, 200], x[3, 5], x[rows - 1, K - 1] = float("inf"), float("nan"), float("-inf")
+    w[140, 300], w[7, 0] = float("-inf"), float("nan")
+    m, held = B.ScaledMatrix(w), U.blocks(w, True)
+    for fp32 in (True, False):
+        got = m.product(x, fp32=fp32)
+        want, bound = U.product(x, held, got.dtype, rows > B.DUO_MAX_ROWS and not fp32)
+        bad = torch.zeros((rows, N), dtype=torch.bool)
+        bad[[1, 3, rows - 1]] = bad[:, [7, 140]] = True
+        assert torch.equal(torch.isnan(got).cpu(), bad)
+        U.close(got.cpu()[~bad], want[~bad], bound[~bad])
